@@ -428,6 +428,228 @@ int chunked_prefill_attention(const void* q, const void* k_blocks, const void* v
                               void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Block tables and slot maps on the device (asynchronous).                  */
+/*                                                                           */
+/* Blocks are handed out on demand (Sec. 3 effect 1).  kv_pool_alloc_seq    */
+/* does it on the host; this call does it where the lengths already are,    */
+/* for a whole batch and without a synchronisation: it gives every sequence */
+/* the blocks its next tokens need, from a ring of free ids in device       */
+/* memory, takes back the blocks of sequences that are over, and writes the */
+/* block tables and, for every new token (a row), its cache slot and its    */
+/* position.                                                                 */
+/*   The ring: free_ids [num_blocks]; free_state_in = {head, count}: the    */
+/* ids free_ids[(head + i) % num_blocks], i < count, are free (a new pool:  */
+/* all ids of a kv_pool, head 0).                                            */
+/*   Sequence s with c = context_lens[s] cached tokens (not counting the    */
+/* new ones), b = n_owned[s] blocks in its table (at least ceil(c / 16),    */
+/* which a smaller value is taken for) and x = new_tokens[s]:               */
+/*     x < 0   the sequence is over: its b table entries go to the end of   */
+/*             the ring, in table order, sequences in batch order; its      */
+/*             context and owned count become 0 (they are free for the next */
+/*             call, not for this one)                                       */
+/*     x >= 0  it needs max(0, ceil((c + x) / 16) - b) blocks.  In batch    */
+/*             order, needs are met while the sum of all needs so far is at */
+/*             most `count`; a sequence that needs none is always met.      */
+/*             granted[s] = 1, context c + x, table entries b and up set to */
+/*             the next ids of the ring.  Else granted[s] = 0 and the       */
+/*             sequence stays as it was.  Refused too, and left out of the  */
+/*             sum: c + x > 16 * max_blocks_per_seq, rows that end past     */
+/*             total_rows, more than 64 * mask_words rows with parents.     */
+/*   Rows: sequence s has rows q_start[s] .. q_start[s+1] (q_start = the    */
+/* running sum of max(x, 0), whether granted or not, cut at total_rows).    */
+/* The rows of a refused sequence have no tokens in the cache: attention's   */
+/* results for them are of no use.                                           */
+/* Row i of s is cached at t = c + i:                                        */
+/*     slots = block_tables[s][t / 16] * 16 + t % 16 (-1 if not granted)     */
+/*     positions = t, or with parents c + (number of ancestors)              */
+/* Rows behind the last sequence (a batch padded to a fixed size) get slot  */
+/* -1, position -1 and an empty mask.                                        */
+/*   parents (may be NULL) makes each sequence's rows a tree of drafted     */
+/* tokens: parents[row] is the index within the sequence of the row's       */
+/* parent, which must come before it; -1 (as any other value) for a child   */
+/* of the cached context.  tree_mask [total_rows, mask_words] 64-bit words, */
+/* bit j % 64 of word j / 64 for row j of the sequence: set for the row and */
+/* its ancestors.                                                            */
+/*                                                                           */
+/*   context_lens, n_owned, new_tokens, granted, context_lens_out,           */
+/*   n_owned_out [batch] int32; free_ids [num_blocks] int32 (updated in      */
+/*   place); free_state_in, free_state_out [2] int32; block_tables [batch,   */
+/*   max_blocks_per_seq] int32 (updated in place; entries from the owned    */
+/*   count on are of no meaning); q_start [batch + 1] int32; slots           */
+/*   [total_rows] int64; positions, parents [total_rows] int32.              */
+/* The outputs context_lens_out, n_owned_out, free_state_out and q_start    */
+/* must not be the inputs (DP_EINVAL).  The updates in place leave what the */
+/* call reads alone, so a call repeated on the same inputs does the same.   */
+/* One launch; nothing is allocated.  batch <= 4096, block_size 16,         */
+/* total_rows and num_blocks <= 2^30, mask_words 0 (no parents) to 4.       */
+/* DP_EINVAL / DP_ENOTSUP for bad arguments (nothing enqueued), DP_EIO if   */
+/* the launch fails.                                                         */
+/* ------------------------------------------------------------------------ */
+typedef struct {
+  int32_t batch;
+  int32_t block_size;
+  int32_t max_blocks_per_seq;
+  int32_t mask_words; /* 64-bit words of a row of tree_mask, 1..4; 0 without parents */
+  int64_t total_rows; /* rows of slots, positions, parents and tree_mask             */
+  int64_t num_blocks; /* ids of the pool: entries of free_ids                        */
+  int64_t reserved;   /* must be 0                                                   */
+} dp_tables_shape;
+
+int kv_tables_step(const int32_t* context_lens, const int32_t* n_owned, const int32_t* new_tokens,
+                   const int32_t* parents, int32_t* free_ids, const int32_t* free_state_in,
+                   int32_t* block_tables, int32_t* context_lens_out, int32_t* n_owned_out,
+                   int32_t* free_state_out, int32_t* q_start, int64_t* slots, int32_t* positions,
+                   int32_t* granted, uint64_t* tree_mask, const dp_tables_shape* shape, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Norm and rotation of queries and keys, with the cache write (device,      */
+/* asynchronous).                                                            */
+/*                                                                           */
+/* What comes before the attention of a step, in one pass over the new      */
+/* tokens' projections.  For row r at position p = positions[r], and each   */
+/* head vector x of q and k:                                                 */
+/*     y = x * w / sqrt(mean(x^2) + eps)     (q_weight or k_weight;          */
+/*                                            y = x without that weight)     */
+/*     the first rotary_dim dimensions of y are turned pair by pair, pair d  */
+/*     = (d, d + rotary_dim / 2), or (2d, 2d + 1) if interleaved, by the     */
+/*     angle whose cosine and sine are cos_sin[p][d] and                     */
+/*     cos_sin[p][rotary_dim / 2 + d]:                                       */
+/*         y_a' = y_a cos - y_b sin,  y_b' = y_b cos + y_a sin               */
+/*     q_out[r, h, :] = y' rounded to bf16                                   */
+/*     k_blocks[blk, g, slot, :] = enc(y' / k_scale[g])                      */
+/*     v_blocks[blk, g, :, slot] = enc(v[r, g, :] / v_scale[g])              */
+/* with blk = slots[r] / 16, slot = slots[r] % 16; enc() rounds to bf16, or */
+/* as in kv_cache_append to e4m3.  All arithmetic is fp32, rounded once.    */
+/* A row whose position is outside [0, n_positions) is left alone            */
+/* altogether; one whose slot is outside [0, 16 * num_blocks) writes q_out   */
+/* and no cache.  Two rows that name the same slot race.                     */
+/*                                                                           */
+/*   q [rows, n_q_heads, 128], k, v [rows, n_kv_heads, 128] bf16, heads      */
+/*   contiguous, rows q_stride, k_stride, v_stride elements apart (slices    */
+/*   of one projection's output, say); strides are multiples of 8            */
+/*   q_weight, k_weight [128] bf16, either may be NULL                       */
+/*   cos_sin [n_positions, rotary_dim] fp32; positions [rows] int32;         */
+/*   slots [rows] int64                                                      */
+/*   q_out [rows, n_q_heads, 128] bf16, contiguous; may be q itself where    */
+/*   q_stride is n_q_heads * 128                                             */
+/*   k_blocks, v_blocks, k_scale, v_scale: as for kv_cache_append            */
+/* q, k, v, weights, cos_sin, q_out and the caches are 16-byte aligned.     */
+/* rotary_dim is a multiple of 16 in [0, 128].  One launch; nothing is      */
+/* allocated.  DP_EINVAL / DP_ENOTSUP for bad arguments (nothing enqueued), */
+/* DP_EIO if the launch fails.                                               */
+/* ------------------------------------------------------------------------ */
+typedef struct {
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 128                                    */
+  int32_t block_size;  /* 16                                     */
+  int32_t kv_dtype;    /* DP_KV_*                                */
+  int32_t rotary_dim;
+  int32_t interleaved; /* 0: pairs (d, d + rotary_dim/2); 1: pairs (2d, 2d+1) */
+  int32_t reserved;    /* must be 0                              */
+  int64_t rows;
+  int64_t num_blocks;
+  int64_t n_positions; /* rows of cos_sin                        */
+  int64_t q_stride;    /* elements from one row to the next      */
+  int64_t k_stride;
+  int64_t v_stride;
+} dp_qk_shape;
+
+int qk_norm_rope_append(const void* q, const void* k, const void* v, const void* q_weight,
+                        const void* k_weight, float eps, const float* cos_sin,
+                        const int32_t* positions, const int64_t* slots, void* q_out, void* k_blocks,
+                        void* v_blocks, const float* k_scale, const float* v_scale,
+                        const dp_qk_shape* shape, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Attention of drafted trees over the paged cache (device, asynchronous).  */
+/*                                                                           */
+/* Speculative decoding checks several drafted tokens of a sequence in one  */
+/* pass; they form a tree, and each may see the committed tokens, its       */
+/* ancestors and itself.  For sequence s with T = context_lens[s] cached    */
+/* tokens (the drafts included: K and V of draft j sit at token T - n + j)  */
+/* and n = q_start[s+1] - q_start[s] drafts, row r = q_start[s] + i:        */
+/*   out[r,h,:] = sum_t softmax_t(scale * q[r,h,:] . K_t) V_t               */
+/*   over t < T - n, and t = T - n + j for every j < n whose bit j % 64 of  */
+/*   tree_mask[r][j / 64] is set                                             */
+/* with K_t, V_t gathered exactly as for paged_decode_attention.  Any bits  */
+/* are allowed: a chain of drafts (bits 0..i), windows, rows that see no    */
+/* draft.  A row that sees no token at all gives zeros.  A cached value of   */
+/* a token that a row does not see never reaches it, finite or not.          */
+/*                                                                           */
+/* Layouts: q, out [total_q, n_q_heads, 128] bf16, rows packed as q_start   */
+/* says; tree_mask [total_q, mask_words] 64-bit words, 8-byte aligned; the  */
+/* rest as for chunked_prefill_attention.  A caller promise: n <= T and     */
+/* n <= 64 * mask_words.  Values that break it are clamped: no access        */
+/* leaves the buffers, rows past the clamped n are left unwritten.           */
+/* Probabilities enter the second product as bf16 (the denominator sums the */
+/* rounded ones); everything else is fp32 until out is rounded.              */
+/*   workspace >= tree_decode_workspace_size(shape) bytes, 256-byte aligned, */
+/* of any content; calls that share one must not overlap in time.           */
+/* Results are deterministic.  At most two launches; nothing is allocated.  */
+/* Supported: head_dim 128, block_size 16, Hq a multiple of Hkv,            */
+/* batch <= 4096, mask_words 1..4, Hq / Hkv <= 1024.                        */
+/* ------------------------------------------------------------------------ */
+typedef struct {
+  int32_t batch;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t block_size;
+  int32_t max_blocks_per_seq;
+  int32_t max_context_len;
+  int32_t kv_dtype;   /* DP_KV_*                              */
+  int32_t mask_words; /* 64-bit words of a row of tree_mask   */
+  int32_t reserved;   /* must be 0                            */
+  int64_t total_q;    /* rows of q, out and tree_mask         */
+  int64_t num_blocks; /* blocks in k_blocks / v_blocks        */
+} dp_tree_shape;
+
+/* Bytes of workspace tree_decode_attention needs for this shape.  Returns 0
+ * for invalid shapes (the reason is in dp_last_error()). */
+size_t tree_decode_workspace_size(const dp_tree_shape* shape);
+
+/* Enqueue the attention on `stream`.  DP_EINVAL / DP_ENOTSUP for bad
+ * arguments, DP_ENOMEM for a short workspace (nothing enqueued); DP_EIO if a
+ * launch fails. */
+int tree_decode_attention(const void* q, const void* k_blocks, const void* v_blocks,
+                          const int32_t* block_tables, const int32_t* context_lens,
+                          const int32_t* q_start, const uint64_t* tree_mask, float scale,
+                          const float* k_scale, const float* v_scale, void* out,
+                          const dp_tree_shape* shape, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Accepted drafts kept in the cache (device, asynchronous).                */
+/*                                                                           */
+/* After the model has checked a tree, one path of it is accepted.  Its     */
+/* tokens lie scattered among the n drafted slots of the cache; this call   */
+/* moves them to the front of those slots, in every layer's cache at once:  */
+/* for sequence s (T, n as for tree_decode_attention) and j < a:            */
+/*   K and V of token T - n + j = those of token T - n + accepted[s][j]     */
+/*   context_lens_out[s] = T - n + a                                         */
+/* a is n_accepted[s], cut at max_accept, at n, and at the first entry that */
+/* is not larger than the one before it or not in [0, n).  n_accepted[s] < 0 */
+/* leaves the sequence alone, context_lens_out[s] = T (for one that          */
+/* kv_tables_step refused: it has rows, but no cached drafts).  Codes are    */
+/* moved as they are.  A token whose block id is outside the pool is not     */
+/* moved.                                                                    */
+/*   k_layers, v_layers  host arrays of n_layers device pointers, caches as */
+/*                       for kv_cache_append, all of one shape, no two the  */
+/*                       same; read during the call only                     */
+/*   accepted [batch, max_accept] int32, n_accepted [batch] int32;          */
+/*   context_lens_out [batch] int32, not context_lens itself                 */
+/*   shape  mask_words is not looked at                                      */
+/* One launch per 64 layers (n_layers >= 1); nothing is allocated.          */
+/* DP_EINVAL / DP_ENOTSUP for bad arguments (nothing enqueued), DP_EIO if a */
+/* launch fails.                                                             */
+/* ------------------------------------------------------------------------ */
+int kv_cache_accept(void* const* k_layers, void* const* v_layers, int32_t n_layers,
+                    const int32_t* block_tables, const int32_t* context_lens, const int32_t* q_start,
+                    const int32_t* accepted, const int32_t* n_accepted, int32_t max_accept,
+                    int32_t* context_lens_out, const dp_tree_shape* shape, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* HBM read probe (device, asynchronous; measurement only).                 */
 /*                                                                           */
 /* Decode attention is bound by the rate at which the cached K and V can be */

@@ -34,7 +34,8 @@ EXPORTS = (
     "route_adapt_default_params", "route_adapt_threshold", "dp_cost_model",
     "paged_decode_workspace_size", "paged_decode_partition_tokens", "paged_decode_attention",
     "paged_decode_attention_noalloc",
-    "kv_cache_append", "chunked_prefill_attention", "dp_hbm_read_probe",
+    "kv_cache_append", "chunked_prefill_attention", "kv_tables_step", "qk_norm_rope_append",
+    "tree_decode_workspace_size", "tree_decode_attention", "kv_cache_accept", "dp_hbm_read_probe",
 )
 
 
@@ -97,6 +98,28 @@ class PrefillShape(ctypes.Structure):
                 ("reserved", ctypes.c_int32), ("total_q", ctypes.c_int64), ("num_blocks", ctypes.c_int64)]
 
 
+class TablesShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("block_size", ctypes.c_int32), ("max_blocks_per_seq", ctypes.c_int32),
+                ("mask_words", ctypes.c_int32), ("total_rows", ctypes.c_int64), ("num_blocks", ctypes.c_int64),
+                ("reserved", ctypes.c_int64)]
+
+
+class QKShape(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block_size", ctypes.c_int32), ("kv_dtype", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("reserved", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("num_blocks", ctypes.c_int64), ("n_positions", ctypes.c_int64), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
+class TreeShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("block_size", ctypes.c_int32),
+                ("max_blocks_per_seq", ctypes.c_int32), ("max_context_len", ctypes.c_int32),
+                ("kv_dtype", ctypes.c_int32), ("mask_words", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("total_q", ctypes.c_int64), ("num_blocks", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -138,6 +161,15 @@ def lib() -> ctypes.CDLL:
         L.kv_cache_append.argtypes = [ctypes.c_void_p] * 8 + [ctypes.POINTER(DecodeShape), ctypes.c_void_p]
         L.chunked_prefill_attention.argtypes = [ctypes.c_void_p] * 6 + [ctypes.c_float] + [ctypes.c_void_p] * 3 + [
             ctypes.POINTER(PrefillShape), ctypes.c_void_p]
+        L.kv_tables_step.argtypes = [ctypes.c_void_p] * 15 + [ctypes.POINTER(TablesShape), ctypes.c_void_p]
+        L.qk_norm_rope_append.argtypes = [ctypes.c_void_p] * 5 + [ctypes.c_float] + [ctypes.c_void_p] * 8 + [
+            ctypes.POINTER(QKShape), ctypes.c_void_p]
+        L.tree_decode_workspace_size.argtypes = [ctypes.POINTER(TreeShape)]
+        L.tree_decode_workspace_size.restype = ctypes.c_size_t
+        L.tree_decode_attention.argtypes = [ctypes.c_void_p] * 7 + [ctypes.c_float] + [ctypes.c_void_p] * 3 + [
+            ctypes.POINTER(TreeShape), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        L.kv_cache_accept.argtypes = [ctypes.c_void_p] * 2 + [ctypes.c_int32] + [ctypes.c_void_p] * 5 + [
+            ctypes.c_int32, ctypes.c_void_p, ctypes.POINTER(TreeShape), ctypes.c_void_p]
         L.dp_hbm_read_probe.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_int64,
                                         ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         _lib = L
@@ -369,6 +401,87 @@ def chunked_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens,
         _stream_ptr(stream)))
 
 
+# ---------------------------------------------------------------- a step that verifies drafted tokens
+
+def tables_shape(batch, max_blocks_per_seq, num_blocks, total_rows, mask_words=0, block_size=16) -> TablesShape:
+    return TablesShape(batch, block_size, max_blocks_per_seq, mask_words, total_rows, num_blocks, 0)
+
+
+def kv_tables_step(context_lens, n_owned, new_tokens, free_ids, free_state, block_tables, context_lens_out,
+                   n_owned_out, free_state_out, q_start, slots, positions, granted, shape: TablesShape, parents=None,
+                   tree_mask=None, stream=None) -> None:
+    """Enqueue one step of the block tables (include/dpool.h, kv_tables_step)."""
+    check(lib().kv_tables_step(
+        context_lens.data_ptr(), n_owned.data_ptr(), new_tokens.data_ptr(),
+        parents.data_ptr() if parents is not None else None, free_ids.data_ptr(), free_state.data_ptr(),
+        block_tables.data_ptr(), context_lens_out.data_ptr(), n_owned_out.data_ptr(), free_state_out.data_ptr(),
+        q_start.data_ptr(), slots.data_ptr(), positions.data_ptr(), granted.data_ptr(),
+        tree_mask.data_ptr() if tree_mask is not None else None, ctypes.byref(shape), _stream_ptr(stream)))
+
+
+def qk_shape(rows, n_q_heads, n_kv_heads, num_blocks, n_positions, rotary_dim=128, interleaved=False, kv_fp8=False,
+             q_stride=None, k_stride=None, v_stride=None, head_dim=128, block_size=16) -> QKShape:
+    """Strides in elements from one row to the next; None: rows lie next to each other."""
+    return QKShape(n_q_heads, n_kv_heads, head_dim, block_size, KV_FP8_E4M3 if kv_fp8 else KV_BF16, rotary_dim,
+                   int(interleaved), 0, rows, num_blocks, n_positions,
+                   n_q_heads * head_dim if q_stride is None else q_stride,
+                   n_kv_heads * head_dim if k_stride is None else k_stride,
+                   n_kv_heads * head_dim if v_stride is None else v_stride)
+
+
+def qk_norm_rope_append(q, k, v, cos_sin, positions, slots, q_out, k_blocks, v_blocks, shape: QKShape, q_weight=None,
+                        k_weight=None, eps=1e-6, k_scale=None, v_scale=None, stream=None) -> None:
+    """Enqueue norm, rotation and cache write of the new tokens (include/dpool.h, qk_norm_rope_append)."""
+    check(lib().qk_norm_rope_append(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), q_weight.data_ptr() if q_weight is not None else None,
+        k_weight.data_ptr() if k_weight is not None else None, float(eps),
+        cos_sin.data_ptr() if cos_sin is not None else None, positions.data_ptr(), slots.data_ptr(),
+        q_out.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(),
+        k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None,
+        ctypes.byref(shape), _stream_ptr(stream)))
+
+
+def tree_shape(batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks, total_q, mask_words=1,
+               kv_fp8=False, head_dim=128, block_size=16) -> TreeShape:
+    return TreeShape(batch, n_q_heads, n_kv_heads, head_dim, block_size, max_blocks_per_seq, max_context_len,
+                     KV_FP8_E4M3 if kv_fp8 else KV_BF16, mask_words, 0, total_q, num_blocks)
+
+
+def tree_workspace_size(shape: TreeShape) -> int:
+    return int(lib().tree_decode_workspace_size(ctypes.byref(shape)))
+
+
+def tree_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, q_start, tree_mask, scale, out,
+                          shape: TreeShape, workspace, k_scale=None, v_scale=None, stream=None) -> None:
+    """Enqueue the attention of drafted trees (include/dpool.h, tree_decode_attention)."""
+    ws_ptr, ws_bytes = _ws(workspace)
+    check(lib().tree_decode_attention(
+        q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
+        q_start.data_ptr(), tree_mask.data_ptr(), float(scale), k_scale.data_ptr() if k_scale is not None else None,
+        v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape), ws_ptr, ws_bytes,
+        _stream_ptr(stream)))
+
+
+class CacheLayers:
+    """The K and V caches of several layers, as kv_cache_accept takes them (keeps the tensors alive)."""
+
+    def __init__(self, k_layers, v_layers):
+        if len(k_layers) != len(v_layers):
+            raise ValueError("as many K as V caches")
+        self.tensors = (list(k_layers), list(v_layers))
+        self.n = len(k_layers)
+        self.k, self.v = ((ctypes.c_void_p * self.n)(*[t.data_ptr() for t in ts]) for ts in self.tensors)
+
+
+def kv_cache_accept(layers: CacheLayers, block_tables, context_lens, q_start, accepted, n_accepted, context_lens_out,
+                    shape: TreeShape, stream=None) -> None:
+    """Enqueue the move of the accepted drafts, accepted [batch, max_accept] (include/dpool.h, kv_cache_accept)."""
+    check(lib().kv_cache_accept(
+        layers.k, layers.v, layers.n, block_tables.data_ptr(), context_lens.data_ptr(), q_start.data_ptr(),
+        accepted.data_ptr(), n_accepted.data_ptr(), accepted.shape[1], context_lens_out.data_ptr(),
+        ctypes.byref(shape), _stream_ptr(stream)))
+
+
 def hbm_read_probe(buf, workgroups, sink, tile_ids=None, stream=None) -> None:
     """Enqueue one read of `buf` (contiguous, or its 4 KiB tiles in `tile_ids` order)."""
     nbytes = buf.numel() * buf.element_size()
@@ -406,4 +519,33 @@ class PagedDecoder:
                  stream=None):
         paged_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, scale, out, self.shape,
                                self.workspace, k_scale, v_scale, stream)
+        return out
+
+
+class TreeDecoder:
+    """Holds one tree-attention shape and its workspace; calling it enqueues the attention.
+
+    Device memory for the workspace comes from torch's allocator once, at
+    construction; each call only marshals pointers into tree_decode_attention.
+    """
+
+    def __init__(self, batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks, total_q,
+                 mask_words=1, kv_fp8=False, device="cuda"):
+        import torch
+        self.shape = tree_shape(batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks,
+                                total_q, mask_words, kv_fp8)
+        ws = tree_workspace_size(self.shape)
+        if ws == 0:
+            raise DpoolError(DP_EINVAL, last_error())
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=device)
+
+    def new_out(self, device="cuda"):
+        import torch
+        s = self.shape
+        return torch.empty((s.total_q, s.n_q_heads, s.head_dim), dtype=torch.bfloat16, device=device)
+
+    def __call__(self, q, k_blocks, v_blocks, block_tables, context_lens, q_start, tree_mask, scale, out, k_scale=None,
+                 v_scale=None, stream=None):
+        tree_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, q_start, tree_mask, scale, out,
+                              self.shape, self.workspace, k_scale, v_scale, stream)
         return out

@@ -1,0 +1,168 @@
+"""Refusals of the operators of a step that verifies drafted tokens (host side only: nothing is launched)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+EINVAL, ENOMEM, ENOTSUP = -22, -12, -95
+P = 4096     # stands for any aligned device pointer; only calls that the host refuses get it
+
+
+def tables(lib, args=(), sh=(), **kw):
+    shape = dict(batch=4, max_blocks_per_seq=8, num_blocks=64, total_rows=10)
+    words = dict(kw).pop("mask_words", 0)
+    s = lib.tables_shape(**dict(shape, **kw))
+    for k, v in dict(sh).items():
+        setattr(s, k, v)
+    names = ["context", "owned", "new", "parents", "ring", "state", "tables", "context_out", "owned_out", "state_out",
+             "q_start", "slots", "positions", "granted", "mask"]
+    vals = {n: P + 256 * i for i, n in enumerate(names)}
+    if not words:
+        vals["parents"] = vals["mask"] = None
+    vals.update(dict(args))
+    return lib.lib().kv_tables_step(*[vals[n] for n in names], ctypes.byref(s), None)
+
+
+@pytest.mark.parametrize("kw,sh,code", [
+    (dict(batch=-1), {}, EINVAL), (dict(batch=4097), {}, ENOTSUP), (dict(block_size=32), {}, ENOTSUP),
+    (dict(max_blocks_per_seq=0), {}, EINVAL), (dict(max_blocks_per_seq=1 << 28), {}, EINVAL),
+    (dict(num_blocks=0), {}, EINVAL), (dict(num_blocks=(1 << 30) + 1), {}, EINVAL),
+    (dict(total_rows=-1), {}, EINVAL), (dict(total_rows=(1 << 30) + 1), {}, EINVAL),
+    (dict(mask_words=5), {}, ENOTSUP), (dict(mask_words=-1), {}, ENOTSUP), ({}, dict(reserved=1), EINVAL)])
+def test_tables_shapes_refused(host_lib, kw, sh, code):
+    assert tables(host_lib, sh=sh, **kw) == code
+    assert host_lib.last_error() != ""
+
+
+@pytest.mark.parametrize("args,words", [
+    (dict(context=None), 0), (dict(owned=None), 0), (dict(new=None), 0), (dict(ring=None), 0), (dict(state=None), 0),
+    (dict(tables=None), 0), (dict(q_start=None), 0), (dict(slots=None), 0), (dict(positions=None), 0),
+    (dict(granted=None), 0), (dict(parents=None), 1), (dict(mask=None), 1), (dict(parents=P), 0),
+    (dict(parents=P, mask=P + 64), 0), (dict(slots=P + 4), 0), (dict(context=P + 2), 0), (dict(mask=P + 4), 1),
+    (dict(context=P, context_out=P), 0), (dict(state=P, state_out=P), 0), (dict(owned=P, owned_out=P), 0),
+    (dict(new=P, q_start=P), 0), (dict(parents=P, positions=P), 1)])
+def test_tables_pointers_refused(host_lib, args, words):
+    assert tables(host_lib, args, mask_words=words) == EINVAL
+    assert host_lib.lib().kv_tables_step(*[P] * 15, None, None) == EINVAL
+
+
+def qk(lib, args=(), sh=(), **kw):
+    s = lib.qk_shape(**dict(dict(rows=4, n_q_heads=8, n_kv_heads=2, num_blocks=64, n_positions=100), **kw))
+    for k, v in dict(sh).items():
+        setattr(s, k, v)
+    fp8 = bool(kw.get("kv_fp8"))
+    vals = dict(q=P, k=P, v=P, qw=None, kw=None, eps=1e-6, cos=P, pos=P, slots=P, out=2 * P, kc=P, vc=P,
+                ks=P if fp8 else None, vs=P if fp8 else None)
+    vals.update(dict(args))
+    return lib.lib().qk_norm_rope_append(*vals.values(), ctypes.byref(s), None)
+
+
+@pytest.mark.parametrize("kw,sh,code", [
+    (dict(head_dim=64), {}, ENOTSUP), (dict(block_size=8), {}, ENOTSUP), ({}, dict(kv_dtype=2), ENOTSUP),
+    ({}, dict(reserved=1), EINVAL), ({}, dict(interleaved=2), EINVAL), (dict(rotary_dim=24), {}, ENOTSUP),
+    (dict(rotary_dim=144), {}, ENOTSUP), (dict(rotary_dim=-16), {}, ENOTSUP),
+    (dict(n_q_heads=0), {}, EINVAL), (dict(n_kv_heads=0), {}, EINVAL), (dict(n_q_heads=65537), {}, EINVAL),
+    (dict(rows=-1), {}, EINVAL), (dict(rows=1 << 40), {}, EINVAL), (dict(num_blocks=0), {}, EINVAL),
+    (dict(n_positions=0), {}, EINVAL), (dict(q_stride=1016), {}, EINVAL), (dict(k_stride=260), {}, EINVAL),
+    (dict(v_stride=-256), {}, EINVAL), (dict(q_stride=1 << 62), {}, EINVAL)])
+def test_qk_shapes_refused(host_lib, kw, sh, code):
+    assert qk(host_lib, sh=sh, **kw) == code
+    assert host_lib.last_error() != ""
+
+
+@pytest.mark.parametrize("args,kw", [
+    (dict(q=None), {}), (dict(k=None), {}), (dict(v=None), {}), (dict(cos=None), {}), (dict(pos=None), {}),
+    (dict(slots=None), {}), (dict(out=None), {}), (dict(kc=None), {}), (dict(vc=None), {}), (dict(q=P + 2), {}),
+    (dict(slots=P + 4), {}), (dict(pos=P + 2), {}), (dict(ks=P, vs=P), {}), (dict(ks=None), dict(kv_fp8=True)),
+    (dict(vs=None), dict(kv_fp8=True)), (dict(out=P), dict(q_stride=2048)), (dict(qw=P + 8), {}),
+    (dict(qw=P, eps=-1.0), {}), (dict(kw=P, eps=float("nan")), {}), (dict(kw=P, eps=float("inf")), {})])
+def test_qk_pointers_refused(host_lib, args, kw):
+    assert qk(host_lib, args, **kw) == EINVAL
+
+
+def tshape(lib, sh=(), **kw):
+    s = lib.tree_shape(**dict(dict(batch=4, n_q_heads=8, n_kv_heads=2, max_blocks_per_seq=8, max_context_len=128,
+                                   num_blocks=64, total_q=10), **kw))
+    for k, v in dict(sh).items():
+        setattr(s, k, v)
+    return s
+
+
+@pytest.mark.parametrize("kw,sh,code", [
+    (dict(head_dim=64), {}, ENOTSUP), (dict(block_size=8), {}, ENOTSUP), ({}, dict(kv_dtype=2), ENOTSUP),
+    ({}, dict(reserved=1), EINVAL), (dict(batch=-1), {}, EINVAL), (dict(batch=4097), {}, ENOTSUP),
+    (dict(mask_words=0), {}, ENOTSUP), (dict(mask_words=5), {}, ENOTSUP), (dict(n_q_heads=9), {}, EINVAL),
+    (dict(n_q_heads=0), {}, EINVAL), (dict(n_kv_heads=-2), {}, EINVAL), (dict(n_q_heads=4096, n_kv_heads=2), {}, ENOTSUP),
+    (dict(n_q_heads=65536, n_kv_heads=65536), {}, ENOTSUP), (dict(max_blocks_per_seq=7), {}, EINVAL),
+    (dict(max_context_len=-1), {}, EINVAL), (dict(num_blocks=0), {}, EINVAL), (dict(num_blocks=1 << 31), {}, EINVAL),
+    (dict(max_context_len=(1 << 30) + 1, max_blocks_per_seq=1 << 27), {}, ENOTSUP), (dict(total_q=-1), {}, EINVAL),
+    (dict(total_q=1 << 31), {}, EINVAL)])
+def test_tree_shapes_refused(host_lib, kw, sh, code):
+    s = tshape(host_lib, sh, **kw)
+    L = host_lib.lib()
+    assert L.tree_decode_workspace_size(ctypes.byref(s)) == 0
+    assert L.tree_decode_attention(*[P] * 7, 1.0, None, None, P, ctypes.byref(s), P, 1 << 30, None) == code
+    assert host_lib.last_error() != ""
+    if code == EINVAL and kw and "total_q" not in kw and "mask_words" not in kw and "n_q_heads" not in kw:
+        assert accept(host_lib, shape=s) in (EINVAL, ENOTSUP)
+
+
+def test_tree_arguments_refused(host_lib):
+    L = host_lib.lib()
+    s, s8 = tshape(host_lib), tshape(host_lib, kv_fp8=True)
+    need = L.tree_decode_workspace_size(ctypes.byref(s))
+    assert need > 0
+
+    def call(shape=s, scale=1.0, ks=None, vs=None, out=P, ws=P, n=1 << 30, **ptr):
+        names = ["q", "k", "v", "tables", "ctx", "q_start", "mask"]
+        vals = [ptr.get(x, P) for x in names]
+        return L.tree_decode_attention(*vals, scale, ks, vs, out, ctypes.byref(shape), ws, n, None)
+
+    for name in ("q", "k", "v", "tables", "ctx", "q_start", "mask"):
+        assert call(**{name: None}) == EINVAL
+        assert call(**{name: P + 2}) == EINVAL
+    assert call(mask=P + 4) == EINVAL and call(q=P + 8) == EINVAL and call(out=None) == EINVAL and call(out=P + 8) == EINVAL
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        assert call(scale=scale) == EINVAL
+    assert call(ks=P, vs=P) == EINVAL and call(shape=s8) == EINVAL and call(shape=s8, ks=P) == EINVAL
+    assert call(ws=None) == EINVAL and call(ws=P + 128) == EINVAL and call(n=need - 1) == ENOMEM
+    assert L.tree_decode_attention(*[None] * 7, 1.0, None, None, None, None, None, 0, None) == EINVAL
+    empty = tshape(host_lib, batch=0)
+    assert L.tree_decode_attention(*[None] * 7, 1.0, None, None, None, ctypes.byref(empty), None, 0, None) == 0
+    empty = tshape(host_lib, total_q=0)
+    assert L.tree_decode_attention(*[None] * 7, 1.0, None, None, None, ctypes.byref(empty), None, 0, None) == 0
+
+
+def accept(lib, shape=None, k=(P, 2 * P), v=(3 * P, 4 * P), n=2, max_accept=4, out=9 * P, **ptr):
+    arr = lambda x: (ctypes.c_void_p * len(x))(*x) if x is not None else None  # noqa: E731
+    names = ["tables", "ctx", "q_start", "accepted", "n_accepted"]
+    vals = [ptr.get(x, P + 64 * i) for i, x in enumerate(names)]
+    shape = tshape(lib) if shape is None else shape
+    return lib.lib().kv_cache_accept(arr(k), arr(v), n, *vals, max_accept, out, ctypes.byref(shape), None)
+
+
+def test_accept_arguments_refused(host_lib):
+    assert accept(host_lib, n=0) == EINVAL and accept(host_lib, n=-1) == EINVAL
+    assert accept(host_lib, max_accept=0) == EINVAL
+    assert accept(host_lib, k=None) == EINVAL and accept(host_lib, v=None) == EINVAL
+    assert accept(host_lib, k=(P, None)) == EINVAL and accept(host_lib, v=(P, P + 2)) == EINVAL
+    for name in ("tables", "ctx", "q_start", "accepted", "n_accepted"):
+        assert accept(host_lib, **{name: None}) == EINVAL and accept(host_lib, **{name: P + 2}) == EINVAL
+    assert accept(host_lib, out=None) == EINVAL and accept(host_lib, out=P + 64) == EINVAL   # the lengths themselves
+    for kw, code in ((dict(head_dim=64), ENOTSUP), (dict(block_size=8), ENOTSUP), (dict(batch=-1), EINVAL),
+                     (dict(batch=4097), ENOTSUP), (dict(n_q_heads=0, n_kv_heads=0), EINVAL),
+                     (dict(max_blocks_per_seq=7), EINVAL), (dict(num_blocks=0), EINVAL), (dict(total_q=-1), EINVAL)):
+        assert accept(host_lib, shape=tshape(host_lib, **kw)) == code
+    assert accept(host_lib, shape=tshape(host_lib, sh=dict(kv_dtype=7))) == ENOTSUP
+    assert accept(host_lib, shape=tshape(host_lib, sh=dict(reserved=7))) == EINVAL
+    assert accept(host_lib, shape=tshape(host_lib, batch=0)) == 0
+    assert host_lib.lib().kv_cache_accept(None, None, 1, *[None] * 5, 1, None, None, None) == EINVAL
+
+
+def test_calls_with_nothing_to_do(host_lib):
+    assert qk(host_lib, dict(q=None, k=None, v=None, out=None, kc=None, vc=None), rows=0) == 0
+
+
+def test_binding_refuses_unequal_layers(host_lib):
+    with pytest.raises(ValueError):
+        host_lib.CacheLayers([np.zeros(1)], [])
