@@ -30,6 +30,7 @@
 #include <cmath>
 #include <cstdint>
 #include <mutex>
+#include <type_traits>
 
 #include "common.h"
 
@@ -47,13 +48,14 @@ constexpr int kMaxWords = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;         // probabilities may reach 2^8 before the reference maximum moves
 constexpr float kMinusBig = -3.0e38f;  // reference maximum of a column without a score (finite: no inf - inf)
-constexpr int kItemCost = 2;           // an item's start and end, in steps (for equal slices)
+constexpr int kItemCost = 4;           // an item's start and end, in steps (for equal slices)
 constexpr int kMinSlice = 4;           // steps of the smallest slice
 
 // The item that a workgroup begins and does not finish
 struct TreePiece {
-  int32_t s, g, c0;
   int32_t last;  // the workgroup with its last piece; -1: none
+  int32_t s, g, c0, r0, n, T;
+  int32_t unused;
 };
 
 struct TreeArgs {
@@ -71,7 +73,7 @@ struct TreeArgs {
   int32_t batch, hq, hkv, group, words;
   int32_t max_blocks, max_ctx, num_blocks_m1, total_q;
   TreePiece* desc;              // [workgroups]
-  float* stat;                  // [2 workgroups, columns, 2] reference maximum and sum
+  float* stat;                  // [2 workgroups, columns, 4] reference maximum, sum, odd
   float* part;                  // [2 workgroups, columns, 128]
 };
 
@@ -95,6 +97,20 @@ __device__ __forceinline__ i32x4 fp8x8_to_bf16(int lo, int hi) {
                __builtin_bit_cast(int, d)};
 }
 
+// A value that is the same in every lane, in a scalar register
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+         (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// Lengths and block tables do not change during a launch: read as constants,
+// an entry that the whole wave needs comes through the scalar cache, whose
+// loads are counted apart from those of K and V (which return in order: a
+// block id among them would hold up every tile behind it).
+typedef const __attribute__((address_space(4))) int32_t* ConstInts;
+__device__ __forceinline__ ConstInts constants(const int32_t* p) { return (ConstInts)(uintptr_t)p; }
+
 // What an item needs to know of its sequence
 struct Seq {
   int r0, n, T;
@@ -102,9 +118,10 @@ struct Seq {
 
 __device__ __forceinline__ Seq sequence(const TreeArgs& a, int s) {
   Seq q;
-  q.r0 = min(max(a.q_start[s], 0), a.total_q);
-  const int r1 = min(max(a.q_start[s + 1], q.r0), a.total_q);
-  q.T = min(max(a.context_lens[s], 0), a.max_ctx);
+  const ConstInts start = constants(a.q_start);
+  q.r0 = min(max(start[s], 0), a.total_q);
+  const int r1 = min(max(start[s + 1], q.r0), a.total_q);
+  q.T = min(max(constants(a.context_lens)[s], 0), a.max_ctx);
   q.n = min(min(r1 - q.r0, q.T), 64 * a.words);
   return q;
 }
@@ -115,80 +132,312 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// ---- equal slices of all the work
+//
+// An item is COLS columns of a sequence and KV head; it costs its KV tiles
+// and kItemCost more for its start and end.  All items in order (sequence, KV
+// head, columns) are cut into one slice of equal cost per workgroup; a piece
+// is what a slice holds of an item.
+
+// A piece: tiles j0 .. j1 of nt
+struct Piece {
+  int s, g, c0, j0, j1, nt;
+  Seq q;
+  int last;  // the workgroup with the item's last piece
+};
+
+template <int COLS, int KT>
+struct Walk {
+  const TreeArgs& a;
+  uint64_t u, u_hi, at, slice;  // next unit, end of the slice, first unit of sequence s
+  int s, wg;
+
+  __device__ __forceinline__ uint32_t units(const Seq& q) const { return (uint32_t)((q.T + KT - 1) / KT + kItemCost); }
+  __device__ __forceinline__ uint32_t items(const Seq& q) const {
+    return (uint32_t)((q.n * a.group + COLS - 1) / COLS * a.hkv);
+  }
+
+  // Finds this workgroup's slice; every thread of the workgroup takes part.
+  // Each scans a few sequences; the one that has the slice's first unit says so.
+  template <int kThreads>
+  __device__ __forceinline__ void begin() {
+    __shared__ uint64_t sums[kThreads / 64];
+    __shared__ uint64_t found_at;
+    __shared__ int found;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, nwg = gridDim.x;
+    // consecutive slices on one XCD (workgroups go to the eight in turn)
+    wg = nwg % 8 == 0 ? (int)(blockIdx.x % 8) * (nwg / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
+    const int per_thread = (a.batch + kThreads - 1) / kThreads;
+    const int s_lo = min(tid * per_thread, a.batch), s_hi = min(s_lo + per_thread, a.batch);
+    uint64_t mine = 0;
+    for (int i = s_lo; i < s_hi; ++i) {
+      const Seq q = sequence(a, i);
+      mine += (uint64_t)units(q) * items(q);
+    }
+    uint64_t upto = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint64_t y = __shfl_up(upto, off);
+      if (lane >= off) upto += y;
+    }
+    if (lane == 63) sums[w] = upto;
+    __syncthreads();
+    uint64_t total = 0, before = 0;
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; ++k) {
+      if (k < w) before += sums[k];
+      total += sums[k];
+    }
+    slice = uniform(max((total + nwg - 1) / nwg, (uint64_t)kMinSlice));
+    u = uniform(min(wg * slice, total));
+    u_hi = uniform(min(u + slice, total));
+    upto += before;
+    if (u < u_hi && mine > 0 && upto - mine <= u && u < upto) {
+      uint64_t x = upto - mine;
+      for (int i = s_lo; i < s_hi; ++i) {
+        const Seq q = sequence(a, i);
+        const uint64_t y = (uint64_t)units(q) * items(q);
+        if (u < x + y) {
+          found = i;
+          found_at = x;
+          break;
+        }
+        x += y;
+      }
+    }
+    __syncthreads();
+    if (u < u_hi) {
+      s = uniform(found);
+      at = uniform(found_at);
+    }
+  }
+
+  // The next piece of the slice that holds a tile; false: there is none.
+  __device__ __forceinline__ bool next(Piece& p) {
+    while (u < u_hi) {
+      const Seq q = sequence(a, s);
+      const uint32_t iu = units(q);
+      const uint64_t end = at + (uint64_t)iu * items(q);
+      if (u >= end) {
+        at = end;
+        ++s;
+        continue;
+      }
+      const uint32_t it = (uint32_t)((u - at) / iu);
+      const uint64_t it0 = at + (uint64_t)it * iu;
+      const uint64_t stop = min(u_hi, it0 + iu);
+      p.j0 = max((int)(u - it0) - kItemCost, 0);
+      p.j1 = max((int)(stop - it0) - kItemCost, 0);
+      u = stop;
+      if (p.j0 >= p.j1) continue;  // nothing but the item's cost
+      const int nct = (q.n * a.group + COLS - 1) / COLS;
+      p.s = s;
+      p.g = (int)it / nct;
+      p.c0 = ((int)it - p.g * nct) * COLS;
+      p.nt = (int)iu - kItemCost;
+      p.q = q;
+      p.last = (int)((it0 + iu - 1) / slice);
+      return true;
+    }
+    return false;
+  }
+};
+
+// The masks of a piece's rows as tiles read them: 64 set bits (committed
+// tokens), the drafts' bits, and clear ones past the last.
+constexpr int kMaskWords = 2 * kMaxWords + 5;
+template <int COLS>
+__device__ __forceinline__ void stage_masks(const TreeArgs& a, const Piece& p, uint32_t (*rows)[kMaskWords]) {
+  const int tok0 = p.c0 / a.group, n_rows = (min(p.c0 + COLS, p.q.n * a.group) - 1) / a.group - tok0 + 1;
+  const int mw = 2 * a.words + 5;
+  for (int i = threadIdx.x; i < n_rows * mw; i += blockDim.x) {
+    const int r = i / mw, k = i - r * mw - 2;
+    uint32_t x = k < 0 ? ~0u : 0u;
+    if (k >= 0 && 32 * k < p.q.n) {
+      x = a.mask[(size_t)(p.q.r0 + tok0 + r) * 2 * a.words + k];
+      if (p.q.n < 32 * k + 32) x &= (1u << (p.q.n - 32 * k)) - 1;
+    }
+    rows[r][k + 2] = x;
+  }
+}
+
+// ---- one wave's columns
+template <int NC>
+struct Columns {
+  i32x4 qf[NC][4];
+  int tok[NC];  // draft of this lane's column, from the piece's first
+  f32x4 acc[NC][8], lsum[NC];
+  float mc[NC], mlim[NC];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int b = 0; b < NC; ++b) {
+      mc[b] = mlim[b] = kMinusBig;
+      lsum[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int nn = 0; nn < 8; ++nn) acc[b][nn] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // Queries of columns first + 16 b + li (idle ones repeat the last).
+  __device__ __forceinline__ void load_q(const TreeArgs& a, const Piece& p, int first) {
+    const int li = threadIdx.x & 15, lj = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int b = 0; b < NC; ++b) {
+      const int cc = min(first + 16 * b + li, p.q.n * a.group - 1), t = cc / a.group;
+      tok[b] = t - p.c0 / a.group;
+      const uint16_t* const x = a.q + ((size_t)(p.q.r0 + t) * a.hq + p.g * a.group + (cc - t * a.group)) * kD;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        qf[b][c] = *(const i32x4*)(x + 32 * c + 8 * lj);
+    }
+  }
+
+  // 32 tokens.  kfrag(m, c), vfrag(nn): operands; this lane's tokens are tl .. tl + 8, eight of them for each lj.
+  // tail: some may be drafts or lie past the end.
+  template <class K, class V>
+  __device__ __forceinline__ void attend(const K& kfrag, const V& vfrag, int tl, bool tail, int pre, float cmul, int words,
+                                         const uint32_t (*rows)[kMaskWords]) {
+    f32x4 z[NC][2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const i32x4 kf = kfrag(m, c);
+#pragma unroll
+        for (int b = 0; b < NC; ++b)
+          z[b][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[b][c]),
+              c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : z[b][m], 0, 0, 0);
+      }
+    __builtin_amdgcn_sched_barrier(0);  // (K's operands are done with before V's are read)
+    i32x4 vf[8];
+#pragma unroll
+    for (int nn = 0; nn < 8; ++nn) vf[nn] = vfrag(nn);
+
+    if (tail) {
+      const int bit = min(tl - pre + 64, 64 * words + 96);
+#pragma unroll
+      for (int b = 0; b < NC; ++b) {
+        const uint32_t* const mr = &rows[tok[b]][bit >> 5];
+        const uint32_t see = (uint32_t)(((uint64_t)mr[1] << 32 | mr[0]) >> (bit & 31));
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (!((see >> x) & 1)) z[b][x >> 2][x & 3] = -INFINITY;
+      }
+    }
+    i32x4 p[NC];
+#pragma unroll
+    for (int b = 0; b < NC; ++b) {
+      float mx = z[b][0][0];
+#pragma unroll
+      for (int x = 1; x < 8; ++x) mx = fmaxf(mx, z[b][x >> 2][x & 3]);
+      if (__builtin_amdgcn_ballot_w64(mx * cmul > mlim[b]) != 0) {
+        const float m_new = fmaxf(mc[b], xor_max(mx) * cmul);
+        if (m_new > mlim[b]) {
+          const float alpha = __builtin_amdgcn_exp2f(mc[b] - m_new);
+          mc[b] = m_new;
+          mlim[b] = m_new + kSlack;
+          lsum[b] *= alpha;
+#pragma unroll
+          for (int nn = 0; nn < 8; ++nn) acc[b][nn] *= alpha;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 8; x += 2) {
+        const float lo = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][x >> 2][x & 3], cmul, -mc[b]));
+        const float hi = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][x >> 2][(x & 3) + 1], cmul, -mc[b]));
+        p[b][x >> 1] = pack_bf16(lo, hi);
+      }
+      bf16x8 ones;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) ones[x] = (__bf16)1.0f;
+      lsum[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, p[b]), lsum[b], 0, 0, 0);
+    }
+#pragma unroll
+    for (int nn = 0; nn < 8; ++nn)
+#pragma unroll
+      for (int b = 0; b < NC; ++b)
+        acc[b][nn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8, vf[nn]), __builtin_bit_cast(bf16x8, p[b]), acc[b][nn], 0, 0, 0);
+  }
+};
+
+// Eight dimensions of a column.  `odd`: among the tiles that hold drafts is a V
+// value that is not finite; the sums left such values out, and here they join
+// the rows that see them (their probabilities are not 0, so a NaN or an
+// infinity is what they come to).
+template <bool FP8>
+__device__ __forceinline__ void store_out(const TreeArgs& a, int s, int g, const Seq& q, int cc, int dim, f32x4 x, f32x4 y,
+                                          bool odd) {
+  constexpr size_t TB = FP8 ? 2048 : 4096;
+  const int t = cc / a.group;
+  if (odd) {
+    const int32_t* const bt = a.block_tables + (size_t)s * a.max_blocks;
+    constexpr int KT = FP8 ? 64 : 32;
+    const int pre = q.T - q.n;
+    for (int tk = pre / KT * KT; tk < q.T; ++tk) {  // from the first tile that holds a draft
+      const int j = tk - pre;
+      if (j >= 0 && !((a.mask[(size_t)(q.r0 + t) * 2 * a.words + (j >> 5)] >> (j & 31)) & 1)) continue;
+      const char* const v = a.v + ((size_t)min(max(bt[tk / kBS], 0), a.num_blocks_m1) * a.hkv + g) * TB;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int i = (dim + e) * kBS + tk % kBS;
+        float f;
+        if constexpr (FP8) f = (((const uint8_t*)v)[i] & 0x7f) == 0x7f ? NAN : 0.f;
+        else f = __uint_as_float((uint32_t)((const uint16_t*)v)[i] << 16);
+        if (!((__float_as_uint(f) & 0x7f800000) == 0x7f800000)) continue;
+        if (e < 4) x[e] += f;
+        else y[e - 4] += f;
+      }
+    }
+  }
+  const i32x4 o = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+  *(i32x4*)(a.out + ((size_t)(q.r0 + t) * a.hq + g * a.group + (cc - t * a.group)) * kD + dim) = o;
+}
+
+// The record that the join of a cut item starts from
+__device__ __forceinline__ void note_start(const TreeArgs& a, const Piece& p, int wg) {
+  TreePiece d;
+  d.last = p.last;
+  d.s = p.s;
+  d.g = p.g;
+  d.c0 = p.c0;
+  d.r0 = p.q.r0;
+  d.n = p.q.n;
+  d.T = p.q.T;
+  d.unused = 0;
+  a.desc[wg] = d;
+}
+
+// ---- many columns: bound by the matrix cores
+//
+// NW waves of 16 NC columns share every tile through LDS.
 template <bool FP8, int NW, int NC>
 __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs a) {
   constexpr int kThreads = NW * 64;
-  constexpr int COLS = 16 * NC * NW;
-  constexpr int SUB = FP8 ? 2 : 1;    // sub-tiles of 32 tokens in a step
-  constexpr int KT = 32 * SUB;        // tokens of a step: 16 KiB of cache
-  constexpr int KB = KT / kBS;        // blocks of a step
-  constexpr int NP = 8 / NW;          // 16-byte pieces of K, and of V, a thread copies per step
+  constexpr int WCOLS = 16 * NC, COLS = WCOLS * NW;
+  constexpr int SUB = FP8 ? 2 : 1;    // 32-token parts of a tile
+  constexpr int KT = 32 * SUB;        // tokens of a tile: 16 KiB of cache
+  constexpr int KB = KT / kBS;        // blocks of a tile
+  constexpr int NP = 8 / NW;          // 16-byte pieces of K, and of V, a thread copies per tile
   constexpr size_t TB = FP8 ? 2048 : 4096;  // bytes of a (block, head) tile
   struct Slot {
     char k[SUB][8192], v[SUB][8192];  // bf16: [32 tokens][128], [2 blocks][128 dims][16 tokens]
   };
   __shared__ __attribute__((aligned(16))) Slot slots[2];
-  __shared__ uint32_t rows[COLS][2 * kMaxWords + 5];
-  __shared__ uint64_t sums[NW];
-  __shared__ uint64_t found_at;
-  __shared__ int found;
+  __shared__ uint32_t rows[COLS][kMaskWords];
+  __shared__ int odd[2];  // 1: a tile with drafts had a V value that is not finite (two pieces in turn)
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, lj = lane >> 4;
-  const int G = a.group;
-  const int nwg = gridDim.x;
-  // consecutive slices on one XCD (workgroups go to the eight in turn)
-  const int wg = nwg % 8 == 0 ? (int)(blockIdx.x % 8) * (nwg / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
+  if (tid < 2) odd[tid] = 0;
+  Walk<COLS, KT> walk{a};
+  walk.template begin<kThreads>();
+  if (tid == 0) a.desc[walk.wg].last = -1;
 
-  // ---- this workgroup's slice of all units
-  const auto item_units = [&](const Seq& q) { return (uint32_t)((q.T + KT - 1) / KT + kItemCost); };
-  const auto items = [&](const Seq& q) { return (uint32_t)((q.n * G + COLS - 1) / COLS * a.hkv); };
-  const int per_thread = (a.batch + kThreads - 1) / kThreads;
-  const int s_lo = min(tid * per_thread, a.batch), s_hi = min(s_lo + per_thread, a.batch);
-  uint64_t mine = 0;
-  for (int s = s_lo; s < s_hi; ++s) {
-    const Seq q = sequence(a, s);
-    mine += (uint64_t)item_units(q) * items(q);
-  }
-  uint64_t upto = mine;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint64_t y = __shfl_up(upto, off);
-    if (lane >= off) upto += y;
-  }
-  if (lane == 63) sums[w] = upto;
-  if (tid == 0) found = -1;
-  __syncthreads();
-  uint64_t total = 0, before = 0;
-#pragma unroll
-  for (int k = 0; k < NW; ++k) {
-    if (k < w) before += sums[k];
-    total += sums[k];
-  }
-  const uint64_t L = max((total + nwg - 1) / nwg, (uint64_t)kMinSlice);
-  const uint64_t u_lo = wg * L, u_hi = min(u_lo + L, total);
-  if (tid == 0) a.desc[wg].last = -1;
-  upto += before;
-  if (u_lo < u_hi && mine > 0 && upto - mine <= u_lo && u_lo < upto) {
-    uint64_t at = upto - mine;
-    for (int s = s_lo; s < s_hi; ++s) {
-      const Seq q = sequence(a, s);
-      const uint64_t u = (uint64_t)item_units(q) * items(q);
-      if (u_lo < at + u) {
-        found = s;
-        found_at = at;
-        break;
-      }
-      at += u;
-    }
-  }
-  __syncthreads();
-  if (u_lo >= u_hi) return;
-  int s = __builtin_amdgcn_readfirstlane(found);
-  uint64_t at = found_at;  // first unit of sequence s
-
-  // ---- geometry of the copies: piece y = NP w + i of a step
+  // geometry of the copies: piece y = NP w + i of a tile
   const int blk_w = w * KB / NW;  // the wave's pieces lie in one block
   int kdst[NP], vdst[NP];         // LDS; e4m3: the second half is 16 bytes on (K: exclusive or)
   uint32_t koff[NP], voff[NP];    // in the block's tile
@@ -220,340 +469,221 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs a) {
 #pragma unroll
   for (int h = 0; h < 2; ++h)
     vro[h] = (lj >> 1) * 4096 + (16 * (li >> 2) + 8 * (h ^ (li >> 3)) + 2 * (li & 3) + (lj & 1)) * 16;
-  bf16x8 ones;
-#pragma unroll
-  for (int x = 0; x < 8; ++x) ones[x] = (__bf16)1.0f;
 
-  // ---- the pieces of the slice
-  uint64_t u = u_lo;
-  for (; u < u_hi; ++s) {
-    Seq q = sequence(a, s);
-    q.r0 = __builtin_amdgcn_readfirstlane(q.r0);
-    q.n = __builtin_amdgcn_readfirstlane(q.n);
-    q.T = __builtin_amdgcn_readfirstlane(q.T);
-    const uint32_t iu = item_units(q), ni = items(q);
-    const uint64_t seq_end = at + (uint64_t)iu * ni;
-    for (; u < u_hi && u < seq_end;) {
-      const uint32_t it = (uint32_t)((u - at) / iu);
-      const uint64_t it0 = at + (uint64_t)it * iu;                // the item's first unit
-      const uint64_t piece_end = min(u_hi, it0 + iu);
-      const int ncols = q.n * G, nct = (ncols + COLS - 1) / COLS;
-      const int nt = (int)iu - kItemCost;
-      const int j0 = max((int)(u - it0) - kItemCost, 0), j1 = max((int)(piece_end - it0) - kItemCost, 0);
-      u = piece_end;
-      if (j0 >= j1) continue;  // (the item's cost units hold no steps)
-      const int g = (int)it / nct, c0 = ((int)it - g * nct) * COLS;
-      const int pre = q.T - q.n;  // committed tokens
-      const int nb = (q.T + kBS - 1) / kBS;
-      const int32_t* const bt = a.block_tables + (size_t)s * a.max_blocks;
-      const bool active = c0 + 16 * NC * w < ncols;  // this wave has columns
-
-      // copies: two steps in registers, two in LDS
-      struct Regs {
-        i32x4 k[NP], v[NP];
-      };
-      Regs rA, rB;
-      const auto block_of = [&](int j) __attribute__((always_inline)) {
-        return bt[min(KB * min(j, j1 - 1) + blk_w, nb - 1)];
-      };
-      const auto load = [&](int id, Regs& r) __attribute__((always_inline)) {
-        const size_t tile = ((size_t)min(max(__builtin_amdgcn_readfirstlane(id), 0), a.num_blocks_m1) * a.hkv + g) * TB;
+  // copies: two tiles in registers, two in LDS
+  struct Regs {
+    i32x4 k[NP], v[NP];
+  };
+  Regs rA, rB;
+  const auto block_of = [&](const Piece& p, int j) __attribute__((always_inline)) {
+    const ConstInts bt = constants(a.block_tables) + (size_t)p.s * a.max_blocks;
+    return bt[min(KB * min(j, p.j1 - 1) + blk_w, (p.q.T + kBS - 1) / kBS - 1)];
+  };
+  const auto load = [&](int id, int g, Regs& x) __attribute__((always_inline)) {
+    const size_t tile = ((size_t)min(max(id, 0), a.num_blocks_m1) * a.hkv + g) * TB;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          r.k[i] = *(const i32x4*)(a.k + tile + koff[i]);
-          r.v[i] = *(const i32x4*)(a.v + tile + voff[i]);
-        }
-      };
-      const auto store = [&](int j, Regs& r) __attribute__((always_inline)) {
-        Slot& to = slots[j & 1];
-        const int t0 = j * KT + blk_w * kBS;
-        if (t0 + kBS > q.T) {  // V of tokens past the end may hold anything: zero
+    for (int i = 0; i < NP; ++i) {
+      x.k[i] = *(const i32x4*)(a.k + tile + koff[i]);
+      x.v[i] = *(const i32x4*)(a.v + tile + voff[i]);
+    }
+  };
+  // V of drafts that is not finite: 0 times it is not 0, and rows that do not
+  // see it must not get it, so it becomes 0 here (store_out() adds it again
+  // where it is seen).  V of slots past the end may hold anything: 0 too.
+  const auto clean = [&](const Seq& q, int j, Regs& x, int turn) __attribute__((always_inline)) {
+    constexpr int N = FP8 ? 4 : 2, BITS = 32 / N;  // values of a word
+    constexpr uint32_t EXP = FP8 ? 0x7f : 0x7f80;  // (e4m3 has no infinities: 0x7f and 0xff are NaN)
+    bool any = false;
 #pragma unroll
-          for (int i = 0; i < NP; ++i)
+    for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              constexpr int N = FP8 ? 4 : 2, BITS = 32 / N;
-              const int first = t0 + (FP8 ? 0 : 8 * (lane & 1)) + N * e;
-              const int keep = min(max(q.T - first, 0), N);
-              r.v[i][e] &= keep == N ? -1 : (1 << (BITS * keep)) - 1;
-            }
-        }
+      for (int e = 0; e < 4; ++e) {
+        const int left = min(max(q.T - (j * KT + blk_w * kBS + (FP8 ? 0 : 8 * (lane & 1)) + N * e), 0), N);
+        const uint32_t y = (uint32_t)x.v[i][e] & (left == N ? ~0u : (1u << (BITS * left)) - 1);
+        uint32_t keep = 0;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          if constexpr (FP8) {
-            *(i32x4*)(to.k[0] + kdst[i]) = fp8x8_to_bf16(r.k[i][0], r.k[i][1]);
-            *(i32x4*)(to.k[0] + (kdst[i] ^ 16)) = fp8x8_to_bf16(r.k[i][2], r.k[i][3]);
-            *(i32x4*)(to.v[0] + vdst[i]) = fp8x8_to_bf16(r.v[i][0], r.v[i][1]);
-            *(i32x4*)(to.v[0] + vdst[i] + 16) = fp8x8_to_bf16(r.v[i][2], r.v[i][3]);
-          } else {
-            *(i32x4*)(to.k[0] + kdst[i]) = r.k[i];
-            *(i32x4*)(to.v[0] + vdst[i]) = r.v[i];
-          }
-        }
-      };
-      int id2;  // block of step j + 2 (in the loop: j + 3) for this wave
-      {
-        const int a0 = block_of(j0), a1 = block_of(j0 + 1);
-        id2 = block_of(j0 + 2);
-        load(a0, rA);
-        load(a1, rB);
+        for (int h = 0; h < N; ++h)
+          if (((y >> (BITS * h)) & EXP) != EXP) keep |= ((1u << BITS) - 1) << (BITS * h);
+        any |= keep != ~0u;
+        x.v[i][e] = (int)(y & keep);
       }
-
-      float cmul = a.scale_log2, vsc = 1.0f;
+    if (any) odd[turn] = 1;
+  };
+  const auto store = [&](int slot, const Regs& x) __attribute__((always_inline)) {
+    Slot& to = slots[slot];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
       if constexpr (FP8) {
-        cmul *= a.k_scale[g];
-        vsc = a.v_scale[g];
+        *(i32x4*)(to.k[0] + kdst[i]) = fp8x8_to_bf16(x.k[i][0], x.k[i][1]);
+        *(i32x4*)(to.k[0] + (kdst[i] ^ 16)) = fp8x8_to_bf16(x.k[i][2], x.k[i][3]);
+        *(i32x4*)(to.v[0] + vdst[i]) = fp8x8_to_bf16(x.v[i][0], x.v[i][1]);
+        *(i32x4*)(to.v[0] + vdst[i] + 16) = fp8x8_to_bf16(x.v[i][2], x.v[i][3]);
+      } else {
+        *(i32x4*)(to.k[0] + kdst[i]) = x.k[i];
+        *(i32x4*)(to.v[0] + vdst[i]) = x.v[i];
       }
-      i32x4 qf[NC][4];
-      int tok[NC];
-      const auto column = [&](int b, int& t) __attribute__((always_inline)) {  // row (draft, head) of q and out
-        const int cc = min(c0 + 16 * (NC * w + b) + li, ncols - 1);  // idle columns repeat the last one
-        t = cc / G;
-        return (size_t)(q.r0 + t) * a.hq + g * G + (cc - t * G);
-      };
-#pragma unroll
-      for (int b = 0; b < NC; ++b) {
-        const uint16_t* const p = a.q + column(b, tok[b]) * kD + 8 * lj;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) qf[b][c] = *(const i32x4*)(p + 32 * c);
-      }
-      // the rows' masks as a tile reads them: 64 set bits (committed tokens),
-      // the drafts' bits, and clear ones past the last
-      const int tok0 = c0 / G, n_rows = (min(c0 + COLS, ncols) - 1) / G - tok0 + 1;
-      const int mw = 2 * a.words + 5;
-      if (j1 * KT > pre) {
-        for (int i = tid; i < n_rows * mw; i += kThreads) {
-          const int r = i / mw, k = i - r * mw - 2;
-          uint32_t x = k < 0 ? ~0u : 0u;
-          if (k >= 0 && 32 * k < q.n) {
-            x = a.mask[(size_t)(q.r0 + tok0 + r) * 2 * a.words + k];
-            if (q.n < 32 * k + 32) x &= (1u << (q.n - 32 * k)) - 1;
-          }
-          rows[r][k + 2] = x;
-        }
-      }
+    }
+  };
 
-      f32x4 acc[NC][8], lsum[NC];
-      float mc[NC], mlim[NC];
-#pragma unroll
-      for (int b = 0; b < NC; ++b) {
-        mc[b] = mlim[b] = kMinusBig;
-        lsum[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int nn = 0; nn < 8; ++nn) acc[b][nn] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
+  // The tiles of all pieces form one stream: while tile i is in work, tile i + 1
+  // goes to LDS and tile i + 3 is asked for, whichever piece they belong to.
+  Piece p, nxt;                  // the piece in work, and the next
+  bool more = walk.next(nxt);    // there is a next
+  if (!more) return;
+  // This wave's blocks of 64 tiles, one a lane, loaded far ahead: loads come
+  // back in order, and scalar ones would be waited for with every LDS read.
+  constexpr int kChunk = 56;
+  int ids, later, first = block_of(nxt, nxt.j0 + lane);  // of tiles base and up, base + kChunk and up; of nxt
+  const auto id_at = [&](int v, int i) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(v, i); };
+  int j, base, end, turn = 1;  // end: tile j1, or one more, so that pieces start in the same registers
+  float cmul, vsc;
+  bool active;  // this wave has columns
+  Columns<NC> st;
 
-      const auto compute = [&](int t0, const char* kt, const char* vt) __attribute__((always_inline)) {
-        f32x4 z[NC][2];
+  // The next piece becomes the one in work: its first tile in slot 0, the next
+  // two on their way in rB and rA (there already if `linked`).
+  const auto enter = [&](bool linked) __attribute__((always_inline)) {
+    p = nxt;
+    turn ^= 1;
+    j = base = p.j0;
+    end = p.j0 + (p.j1 - p.j0 + 1) / 2 * 2;
+    ids = first;
+    if (!linked) {
+      load(id_at(ids, 0), p.g, rA);
+      load(id_at(ids, 1), p.g, rB);
+    }
+    st.load_q(a, p, p.c0 + WCOLS * w);
+    active = p.c0 + WCOLS * w < p.q.n * a.group;
+    more = walk.next(nxt);
+    if (more) first = block_of(nxt, nxt.j0 + lane);
+    later = block_of(p, base + kChunk + lane);
+    cmul = a.scale_log2;
+    vsc = 1.0f;
+    if constexpr (FP8) {
+      cmul *= a.k_scale[p.g];
+      if (cmul == 0.f) cmul = 1e-37f;  // (0 times the -inf of a hidden token is not -inf)
+      vsc = a.v_scale[p.g];
+    }
+    stage_masks<COLS>(a, p, rows);
+    st.clear();
+    if (!linked) {
+      if (p.j0 >= (p.q.T - p.q.n) / KT) clean(p.q, p.j0, rA, turn);
+      store(0, rA);
+      load(id_at(ids, 2), p.g, rA);
+    }
+    // Block ids are waited for here, once (the masks' loads behind them were
+    // already): else the compiler would wait for all loads in every step.
+    __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0)
+    lds_barrier();
+    if (tid == 0) odd[turn ^ 1] = 0;  // (every wave has left the piece before)
+  };
+  const auto step = [&](int slot, Regs& x) __attribute__((always_inline)) {
+    const int pre = p.q.T - p.q.n;  // committed tokens; tiles before pre / KT hold no others
+    if (j + 1 < end) {
+      if (j + 1 >= pre / KT) clean(p.q, j + 1, x, turn);
+    } else if (more && end - p.j0 >= 4 && nxt.j0 >= (nxt.q.T - nxt.q.n) / KT) {
+      clean(nxt.q, nxt.j0, x, turn ^ 1);
+    }
+    store(slot ^ 1, x);
+    const bool own = j + 3 < end || !more;
+    load(own ? id_at(ids, min(j + 3, end - 1) - base) : id_at(first, j + 3 - end), own ? p.g : nxt.g, x);
+    if (active && j < p.j1) {
+      const Slot& sl = slots[slot];
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+      for (int y = 0; y < SUB; ++y)
+        st.attend([&](int m, int c) __attribute__((always_inline)) { return *(const i32x4*)(sl.k[y] + kro[c] + 1024 * m); },
+                  [&](int nn) __attribute__((always_inline)) {
+                    return *(const i32x4*)(sl.v[y] + vro[nn & 1] + 1024 * (nn >> 1));
+                  },
+                  j * KT + 32 * y + 8 * lj, j * KT + 32 * y + 32 > pre, pre, cmul, a.words, rows);
+    }
+    lds_barrier();
+    ++j;
+  };
+  // Results: this lane holds dims 32 (nn / 2) + 8 lj + 4 (nn % 2) + e of its columns.
+  const auto finish = [&]() __attribute__((always_inline)) {
+    const bool whole = p.j0 == 0 && p.j1 == p.nt;
+    const bool odd_v = odd[turn] != 0;
+    if (!whole && p.j0 == 0 && tid == 0) note_start(a, p, walk.wg);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const i32x4 kf = *(const i32x4*)(kt + kro[c] + 1024 * m);
+    for (int b = 0; b < NC; ++b) {
+      const int col = WCOLS * w + 16 * b + li;
+      if (p.c0 + col >= p.q.n * a.group) continue;
+      if (whole) {
+        const float l = st.lsum[b][0];
+        const float inv = l == 0.f ? 0.f : vsc / l;  // a row that sees no token: zeros
 #pragma unroll
-            for (int b = 0; b < NC; ++b)
-              z[b][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  __builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[b][c]),
-                  c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : z[b][m], 0, 0, 0);
-          }
-        i32x4 vf[8];
-#pragma unroll
-        for (int nn = 0; nn < 8; ++nn) vf[nn] = *(const i32x4*)(vt + vro[nn & 1] + 1024 * (nn >> 1));
-
-        // this lane's tokens: t0 + 8 lj + 4 m + e
-        const int tl = t0 + 8 * lj;
-        const bool tail = t0 + 32 > pre;
-        uint32_t odd = 0;  // this lane's tokens with a V value that is not finite
-        uint32_t see[NC];
-        if (tail) {
-          const int bit = min(tl - pre + 64, 64 * a.words + 96);
-#pragma unroll
-          for (int b = 0; b < NC; ++b) {
-            const uint32_t* const mr = &rows[tok[b] - tok0][bit >> 5];
-            see[b] = (uint32_t)(((uint64_t)mr[1] << 32 | mr[0]) >> (bit & 31)) & 0xff;
-#pragma unroll
-            for (int x = 0; x < 8; ++x)
-              if (!((see[b] >> x) & 1)) z[b][x >> 2][x & 3] = -INFINITY;
-          }
-#pragma unroll
-          for (int nn = 0; nn < 8; ++nn)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t x = (uint32_t)vf[nn][e];
-              const bool lo = (x & 0x7f80) == 0x7f80, hi = (x & 0x7f800000) == 0x7f800000;
-              odd |= (lo ? 1u : 0u) << (2 * e) | (hi ? 2u : 0u) << (2 * e);
-              vf[nn][e] = (int)(x & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u)));
-            }
-        }
-        i32x4 p[NC];
-#pragma unroll
-        for (int b = 0; b < NC; ++b) {
-          float mx = z[b][0][0];
-#pragma unroll
-          for (int x = 1; x < 8; ++x) mx = fmaxf(mx, z[b][x >> 2][x & 3]);
-          if (__builtin_amdgcn_ballot_w64(mx * cmul > mlim[b]) != 0) {
-            const float m_new = fmaxf(mc[b], xor_max(mx) * cmul);
-            if (m_new > mlim[b]) {
-              const float alpha = __builtin_amdgcn_exp2f(mc[b] - m_new);
-              mc[b] = m_new;
-              mlim[b] = m_new + kSlack;
-              lsum[b] *= alpha;
-#pragma unroll
-              for (int nn = 0; nn < 8; ++nn) acc[b][nn] *= alpha;
-            }
-          }
-#pragma unroll
-          for (int x = 0; x < 8; x += 2) {
-            float lo = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][x >> 2][x & 3], cmul, -mc[b]));
-            float hi = __builtin_amdgcn_exp2f(__builtin_fmaf(z[b][x >> 2][(x & 3) + 1], cmul, -mc[b]));
-            if (tail) {  // (a key scale of 0 makes -inf a NaN)
-              if (!((see[b] >> x) & 1)) lo = 0.f;
-              if (!((see[b] >> (x + 1)) & 1)) hi = 0.f;
-            }
-            p[b][x >> 1] = pack_bf16(lo, hi);
-          }
-          lsum[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, p[b]), lsum[b], 0, 0, 0);
-        }
+        for (int nn = 0; nn < 8; nn += 2)
+          store_out<FP8>(a, p.s, p.g, p.q, p.c0 + col, 16 * nn + 8 * lj, st.acc[b][nn] * inv, st.acc[b][nn + 1] * inv, odd_v);
+      } else {
+        const size_t rec = (size_t)(2 * walk.wg + (p.j0 == 0)) * COLS + col;
+        if (lj == 0) *(f32x4*)(a.stat + 4 * rec) = f32x4{st.mc[b], st.lsum[b][0], odd_v ? 1.f : 0.f, 0.f};
 #pragma unroll
         for (int nn = 0; nn < 8; ++nn)
-#pragma unroll
-          for (int b = 0; b < NC; ++b)
-            acc[b][nn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, vf[nn]), __builtin_bit_cast(bf16x8, p[b]), acc[b][nn], 0, 0, 0);
-
-        // the values left out above, for the columns that see them
-        if (tail && __builtin_amdgcn_ballot_w64(odd != 0) != 0) {
-          for (int x = 0; x < 32; ++x) {
-            const int src = x >> 3, bit = x & 7;  // the row of lanes that holds token t0 + x
-            if (__ballot(lj == src && ((odd >> bit) & 1)) == 0) continue;
-            const char* const col = vt + (x >> 4) * 4096;
-#pragma unroll
-            for (int b = 0; b < NC; ++b) {
-              // this column's probability of the token, from the lane that has it
-              const uint32_t sees = __shfl(see[b], 16 * src + li);
-              int pw = 0;
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (bit >> 1 == e) pw = p[b][e];
-              pw = __shfl(pw, 16 * src + li);
-              const float pr = (bit & 1) ? __uint_as_float((uint32_t)pw & 0xffff0000u)
-                                         : __uint_as_float((uint32_t)pw << 16);
-#pragma unroll
-              for (int nn = 0; nn < 8; ++nn)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int d = 8 * lj + 4 * (nn & 1) + e;  // dim 32 (nn / 2) + d
-                  const int piece = (2 * d + ((x >> 3) & 1)) ^ ((d >> 4) & 1) << 3;
-                  const uint32_t c = *(const uint16_t*)(col + (nn >> 1) * 1024 + piece * 16 + (x & 7) * 2);
-                  if (((sees >> bit) & 1) && (c & 0x7f80) == 0x7f80) acc[b][nn][e] += pr * __uint_as_float(c << 16);
-                }
-            }
-          }
-        }
-      };
-
-      const auto step = [&](int j, Regs& r) __attribute__((always_inline)) {
-        // step j + 1 to LDS (its loads are two steps old), step j + 3 into the registers
-        store(j + 1, r);
-        const int id = id2;
-        id2 = block_of(j + 4);
-        load(id, r);
-        if (active) {
-          const Slot& sl = slots[j & 1];
-#pragma unroll
-          for (int x = 0; x < SUB; ++x) compute(j * KT + 32 * x, sl.k[x], sl.v[x]);
-        }
-        lds_barrier();
-      };
-      store(j0, rA);
-      {
-        const int id = id2;
-        id2 = block_of(j0 + 3);
-        load(id, rA);
+          *(f32x4*)(a.part + rec * kD + 32 * (nn >> 1) + 8 * lj + 4 * (nn & 1)) = st.acc[b][nn];
       }
-      lds_barrier();
-      int j = j0;
-      for (; j + 1 < j1; j += 2) {
-        step(j, rB);
-        step(j + 1, rA);
-      }
-      if (j < j1) step(j, rB);
-
-      // ---- results: this lane holds dims 32 (nn / 2) + 8 lj + 4 (nn % 2) + e of its columns
-      const bool whole = j0 == 0 && j1 == nt;
-      const int slot = 2 * wg + (j0 == 0);
-      if (!whole && j0 == 0 && tid == 0) {
-        TreePiece d;
-        d.s = s;
-        d.g = g;
-        d.c0 = c0;
-        d.last = (int)((it0 + iu - 1) / L);
-        a.desc[wg] = d;
-      }
-#pragma unroll
-      for (int b = 0; b < NC; ++b) {
-        const int cl = 16 * (NC * w + b) + li;
-        if (c0 + cl >= ncols) continue;
-        int t;
-        const size_t row = column(b, t);
-        if (whole) {
-          const float l = lsum[b][0];
-          const float inv = l == 0.f ? 0.f : vsc / l;  // a row that sees no token: zeros
-#pragma unroll
-          for (int nn = 0; nn < 8; nn += 2) {
-            const f32x4 x = acc[b][nn] * inv, y = acc[b][nn + 1] * inv;
-            const i32x4 o = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
-            *(i32x4*)(a.out + row * kD + 16 * nn + 8 * lj) = o;
-          }
-        } else {
-          const size_t rec = (size_t)slot * COLS + cl;
-          if (lj == 0) {
-            a.stat[2 * rec] = mc[b];
-            a.stat[2 * rec + 1] = lsum[b][0];
-          }
-#pragma unroll
-          for (int nn = 0; nn < 8; ++nn)
-            *(f32x4*)(a.part + rec * kD + 32 * (nn >> 1) + 8 * lj + 4 * (nn & 1)) = acc[b][nn];
-        }
-      }
-      // (the next piece's first writes to LDS follow the last step's barrier; its
-      // masks are read only after its first barrier)
     }
-    at = seq_end;
+  };
+  for (bool linked = false;;) {
+    enter(linked);
+    while (true) {
+      const int stop = min(base + kChunk, end);
+      do {
+        step(0, rB);
+        step(1, rA);
+      } while (j < stop);
+      if (j >= end) break;
+      ids = later;
+      base += kChunk;
+      later = block_of(p, base + kChunk + lane);
+    }
+    finish();
+    if (!more) break;
+    linked = end - p.j0 >= 4;
   }
 }
 
 // Joins the pieces of cut items: out = sum_p o_p 2^(m_p - M) / sum_p l_p 2^(m_p - M).
-// One workgroup per 16 columns of one workgroup's unfinished item; sixteen lanes a column.
+// One workgroup per 16 columns of one workgroup's unfinished item; sixteen lanes
+// a column.  Bound by latency: the first two pieces' places follow from the
+// workgroup's index, so they are loaded beside the note that says whether they
+// count (they lie inside the workspace whatever it says).
+template <bool FP8>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int cols) {
-  const int wg = blockIdx.x;
+  const int wg = blockIdx.x, next = min(wg + 1, (int)gridDim.x - 1);
+  const int col = blockIdx.y * 16 + (threadIdx.x >> 4), dim = (threadIdx.x & 15) * 8;
+  struct Sums {
+    f32x4 ml, x, y;
+  };
+  const auto read = [&](int slot) __attribute__((always_inline)) {
+    const size_t rec = (size_t)slot * cols + col;
+    return Sums{*(const f32x4*)(a.stat + 4 * rec), *(const f32x4*)(a.part + rec * kD + dim),
+                *(const f32x4*)(a.part + rec * kD + dim + 4)};
+  };
+  const Sums s0 = read(2 * wg + 1), s1 = read(2 * next);
   const TreePiece d = a.desc[wg];
   if (d.last < 0) return;
-  const int G = a.group;
-  const Seq q = sequence(a, d.s);
-  const int col = blockIdx.y * 16 + (threadIdx.x >> 4), dim = (threadIdx.x & 15) * 8;
+  const Seq q{d.r0, d.n, d.T};
   const int cc = d.c0 + col;
-  if (cc >= q.n * G) return;
-  const float vsc = a.v_scale ? a.v_scale[d.g] : 1.0f;
-  float m = kMinusBig, l = 0.f;
-  f32x4 o0 = {0.f, 0.f, 0.f, 0.f}, o1 = o0;
-  for (int p = wg; p <= d.last; ++p) {
-    const size_t rec = (size_t)(2 * p + (p == wg)) * cols + col;
-    const float mp = a.stat[2 * rec], lp = a.stat[2 * rec + 1];
-    const f32x4 x = *(const f32x4*)(a.part + rec * kD + dim), y = *(const f32x4*)(a.part + rec * kD + dim + 4);
-    const float mn = fmaxf(m, mp);
-    const float f = __builtin_amdgcn_exp2f(m - mn), fp = __builtin_amdgcn_exp2f(mp - mn);
-    l = l * f + lp * fp;
-    o0 = o0 * f + x * fp;
-    o1 = o1 * f + y * fp;
+  if (cc >= q.n * a.group) return;
+  const float vsc = FP8 ? a.v_scale[d.g] : 1.0f;
+  float m = s0.ml[0], l = s0.ml[1];
+  bool odd = s0.ml[2] != 0.f;
+  f32x4 o0 = s0.x, o1 = s0.y;
+  const auto add = [&](const Sums& s) __attribute__((always_inline)) {
+    const float mn = fmaxf(m, s.ml[0]);
+    const float f = __builtin_amdgcn_exp2f(m - mn), fs = __builtin_amdgcn_exp2f(s.ml[0] - mn);
+    odd |= s.ml[2] != 0.f;
+    l = l * f + s.ml[1] * fs;
+    o0 = o0 * f + s.x * fs;
+    o1 = o1 * f + s.y * fs;
     m = mn;
-  }
+  };
+  add(s1);
+#pragma unroll 4
+  for (int p = wg + 2; p <= d.last; ++p) add(read(2 * p));
   const float inv = l == 0.f ? 0.f : vsc / l;
-  o0 *= inv;
-  o1 *= inv;
-  const int t = cc / G;
-  const i32x4 o = {pack_bf16(o0[0], o0[1]), pack_bf16(o0[2], o0[3]), pack_bf16(o1[0], o1[1]), pack_bf16(o1[2], o1[3])};
-  *(i32x4*)(a.out + ((size_t)(q.r0 + t) * a.hq + d.g * G + (cc - t * G)) * kD + dim) = o;
+  store_out<FP8>(a, d.s, d.g, q, cc, dim, o0 * inv, o1 * inv, odd);
 }
 
 }  // namespace dpool_tree
@@ -612,27 +742,32 @@ int compute_units() {
 
 // Which kernel a call takes, and its workspace
 struct Plan {
-  int waves, blocks;  // of a workgroup; 16-column blocks of a wave
+  int kind;        // columns of an item and how its waves work, see launch_plan()
+  int cols;
   int workgroups;
-  int cols() const { return 16 * waves * blocks; }
   size_t stat_at() const { return ((size_t)workgroups * sizeof(TreePiece) + 255) & ~(size_t)255; }
-  size_t part_at() const { return stat_at() + (((size_t)workgroups * 4 * cols() * sizeof(float) + 255) & ~(size_t)255); }
-  size_t bytes() const { return part_at() + (size_t)workgroups * 2 * cols() * kD * sizeof(float); }
+  size_t part_at() const { return stat_at() + (((size_t)workgroups * 8 * cols * sizeof(float) + 255) & ~(size_t)255); }
+  size_t bytes() const { return part_at() + (size_t)workgroups * 2 * cols * kD * sizeof(float); }
 };
 
 Plan plan(const dp_tree_shape* sh) {
   const int64_t group = sh->n_q_heads / sh->n_kv_heads;
-  const int64_t most = std::min<int64_t>(sh->total_q, 64 * sh->mask_words) * group;  // columns of the largest tree
+  const int64_t per_seq = (sh->total_q * group + std::max(sh->batch, 1) - 1) / std::max(sh->batch, 1);
   const int cus = compute_units();
-  if (most <= 64) return Plan{4, 1, 2 * cus};
-  if (most <= 128) return Plan{4, 2, 2 * cus};
-  return Plan{8, 2, cus};
+  if (per_seq <= 64) return Plan{0, 64, 2 * cus};
+  if (per_seq <= 128) return Plan{1, 128, 2 * cus};
+  return Plan{2, 256, cus};
 }
 
-template <int NW, int NC>
-void launch(const TreeArgs& a, bool fp8, int workgroups, hipStream_t st) {
-  if (fp8) hipLaunchKernelGGL((tree_kernel<true, NW, NC>), dim3(workgroups), dim3(NW * 64), 0, st, a);
-  else hipLaunchKernelGGL((tree_kernel<false, NW, NC>), dim3(workgroups), dim3(NW * 64), 0, st, a);
+template <bool FP8>
+void launch_plan(const Plan& pl, const TreeArgs& a, hipStream_t st) {
+  const dim3 grid(pl.workgroups);
+  switch (pl.kind) {
+    case 0: hipLaunchKernelGGL((tree_kernel<FP8, 4, 1>), grid, dim3(256), 0, st, a); break;
+    case 1: hipLaunchKernelGGL((tree_kernel<FP8, 4, 2>), grid, dim3(256), 0, st, a); break;
+    default: hipLaunchKernelGGL((tree_kernel<FP8, 8, 2>), grid, dim3(512), 0, st, a); break;
+  }
+  hipLaunchKernelGGL(tree_merge_kernel<FP8>, dim3(pl.workgroups, pl.cols / 16), dim3(256), 0, st, a, pl.cols);
 }
 
 }  // namespace
@@ -698,10 +833,8 @@ extern "C" int tree_decode_attention(const void* q, const void* k_blocks, const 
   a.part = (float*)((char*)workspace + pl.part_at());
   (void)hipGetLastError();
   hipStream_t st = (hipStream_t)stream;
-  if (pl.waves == 8) launch<8, 2>(a, fp8, pl.workgroups, st);
-  else if (pl.blocks == 2) launch<4, 2>(a, fp8, pl.workgroups, st);
-  else launch<4, 1>(a, fp8, pl.workgroups, st);
-  hipLaunchKernelGGL(tree_merge_kernel, dim3(pl.workgroups, pl.cols() / 16), dim3(256), 0, st, a, pl.cols());
+  if (fp8) launch_plan<true>(pl, a, st);
+  else launch_plan<false>(pl, a, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(DP_EIO, "tree_decode_attention: kernel launch failed: %s", hipGetErrorString(e));
   return DP_OK;

@@ -235,3 +235,21 @@ def test_key_scale_of_zero(gpu_lib):
     ref, bound = tree.tree_attention(w.q_bits, w.k_store.dense(), w.v_store.dense(), w.block_tables, w.context_lens,
                                      w.meta["q_start"], mask, w.scale, "fp8_e4m3", w.k_scale, w.v_scale)
     assert (np.abs(got - ref) <= bound).all()
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("T,n,t", [(70, 3, 66), (70, 3, 64), (70, 3, 2), (40, 8, 31), (33, 1, 0), (2500, 4, 2495), (2500, 4, 700)])
+def test_committed_values_that_are_not_finite(gpu_lib, T, n, t, fmt):
+    """A committed token's V that is not finite reaches every row, wherever it lies beside the drafts."""
+    note(f"tree, committed token {t} of {T} not finite, {fmt}")
+    w = workloads.make_prefill([(n, T), (n, T)], 4, 2, c_max=T, kv_format=fmt, seed=61)
+    mask = tree_masks(np.random.default_rng(3), [n, n], 1, "tree")
+    d = workloads.to_device(w)
+    clean = call(gpu_lib, w, d, mask, 1)
+    V = w.v_store.dense().copy()
+    V[w.block_tables[1][t // 16], 0, 5:7, t % 16] = 0x7FC0 if fmt == "bf16" else 0x7F
+    d["v"] = (torch.from_numpy(V.view(np.int16)) if fmt == "bf16" else torch.from_numpy(V))[None].cuda()
+    got = call(gpu_lib, w, d, mask, 1)
+    hit = np.zeros(got.shape, bool)
+    hit[n:, :2, 5:7] = True
+    assert np.isnan(got[hit]).all() and np.array_equal(got[~hit], clean[~hit])
