@@ -27,7 +27,7 @@ constexpr int kBS = 16;
 constexpr int kWaves = 4;
 constexpr int kMaxLayers = 64;  // per launch: their addresses are kernel arguments
 constexpr int kMaxBatch = 4096;
-constexpr int kMoves = 4;       // moves in flight together
+constexpr int kMoves = 8;       // moves in flight together
 
 struct AcceptArgs {
   char* k[kMaxLayers];
@@ -96,8 +96,8 @@ __global__ __launch_bounds__(kWaves * 64) void kv_accept_kernel(AcceptArgs a) {
           const size_t tile = ((size_t)(from / kBS) * a.hkv + g) * (kBS * kD);
           const int slot = (int)(from % kBS);
           kv[i] = *(const Pair*)(kl + tile + slot * kD + 2 * lane);
-          v0[i] = vl[tile + (2 * lane) * kBS + slot];
-          v1[i] = vl[tile + (2 * lane + 1) * kBS + slot];
+          v0[i] = vl[tile + lane * kBS + slot];
+          v1[i] = vl[tile + (lane + 64) * kBS + slot];
         }
       }
 #pragma unroll
@@ -106,8 +106,8 @@ __global__ __launch_bounds__(kWaves * 64) void kv_accept_kernel(AcceptArgs a) {
           const size_t tile = ((size_t)(to[i] / kBS) * a.hkv + g) * (kBS * kD);
           const int slot = (int)(to[i] % kBS);
           *(Pair*)(kl + tile + slot * kD + 2 * lane) = kv[i];
-          vl[tile + (2 * lane) * kBS + slot] = v0[i];
-          vl[tile + (2 * lane + 1) * kBS + slot] = v1[i];
+          vl[tile + lane * kBS + slot] = v0[i];
+          vl[tile + (lane + 64) * kBS + slot] = v1[i];
         }
       }
     }
