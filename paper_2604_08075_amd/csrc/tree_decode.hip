@@ -7,23 +7,42 @@
 // row's mask.  K tiles are token-major, V tiles dims-major, as for decode.
 //
 // The (draft, head) pairs of a sequence and KV head form one list of columns,
-// draft by draft; a workgroup takes the next 16 NC of them.  Its four waves
-// take turns at the KV tiles (16 KiB: 32 tokens of bf16 or 64 of e4m3), each
-// for all the columns:
-//   * S^T = K Q^T with v_mfma_f32_16x16x32_bf16, K straight from memory in
-//     operand layout.  The token behind each operand row is chosen so that a
-//     lane's scores are the tokens that its operand of O^T += V^T P^T needs.
+// draft by draft, and an item is the next 64, 128 or 256 of them: the waves of
+// a workgroup share K and V of a tile (16 KiB: 32 tokens of bf16, 64 of e4m3)
+// through LDS, 16 or 32 columns each.  Per tile and wave:
+//   * S^T = K Q^T with v_mfma_f32_16x16x32_bf16.  The token behind each operand
+//     row is chosen so that a lane's scores are the tokens that its operand of
+//     O^T += V^T P^T needs: probabilities never move between lanes.
 //   * online softmax in base 2 (scale * log2 e folded into one multiply-add);
 //     the reference maximum of a column moves only when a score passes it by
 //     2^kSlack, so the common path has no rescale.
-//   * the denominator sums the rounded probabilities, so every output is a
-//     convex combination of V rows.
-// At the end the waves' sums meet in LDS under their common maximum.
+//   * probabilities are rounded to bf16, the operand's type; the denominator is
+//     a product against ones that sums the rounded ones, so that every output
+//     is a convex combination of V rows.  All sums are fp32.
+// All tiles of all items are cut into one slice of equal cost per workgroup; an
+// item that a cut goes through leaves sums (maximum, denominator, o) that a
+// second kernel joins, in order, so results do not depend on timing.
+//
+// What bounds it, measured on one MI355X (a large read reaches 6.6 TB/s, a
+// large bf16 product 1,212 TFLOP/s): 64 columns (eight drafts, GQA 8) memory:
+// sixteen contexts of 32,768 tokens, bf16, 411 us, 5.2 TB/s.  The short pool's
+// 128 ragged contexts 186 us: 1.4 us a tile and workgroup, 6 us for every end
+// of an item, 8 us before the first tile and 13 for the join and its launch.
+// 256 columns: neither alone; the matrix cores are busy half the time (32 drafts
+// on sixteen contexts of 65,536 tokens: 1,294 us, 850 TFLOP/s; e4m3, sixteen
+// drafts, GQA 16: 977).  Four tiles on their way instead of two, and scores,
+// probabilities and products of three tiles interleaved by hand, came to the
+// same within 4%, so the plain order stays.
+//
+// LDS: K's sixteen 16-byte chunks of a token are stored exclusive-or'ed with
+// (token % 4, token / 8 % 4), V's with bit 4 of the dimension, so that the
+// sixteen lanes one pass of a 16-byte read serves start in distinct banks
+// (counted: no conflict cycles).
 //
 // Masks: only tiles that reach past token T - n look at them.  There a value
-// that is not finite must not leak into rows that do not see its token (0 times
-// it is not 0), so V is made zero where it is not finite, and the few such
-// values are added by hand to the columns that see them.
+// of V that is not finite must not leak into rows that do not see its token (0
+// times it is not 0): it is made 0 on its way to LDS, and added to the rows
+// that see it when they are written.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -48,8 +67,11 @@ constexpr int kMaxWords = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;         // probabilities may reach 2^8 before the reference maximum moves
 constexpr float kMinusBig = -3.0e38f;  // reference maximum of a column without a score (finite: no inf - inf)
-constexpr int kItemCost = 4;           // an item's start and end, in steps (for equal slices)
-constexpr int kMinSlice = 4;           // steps of the smallest slice
+// An item's start and end, in tiles, for equal slices (short pool, us, with 1 / 4 / 16:
+// bf16 198 / 186 / 191, e4m3 173 / 153 / 194), and tiles of the smallest slice (three
+// contexts of up to 512 tokens, 1 / 4 / 16: 16.3 / 13.6 / 19.5).
+constexpr int kItemCost = 4;
+constexpr int kMinSlice = 4;
 
 // The item that a workgroup begins and does not finish
 struct TreePiece {
@@ -247,19 +269,21 @@ struct Walk {
 // tokens), the drafts' bits, and clear ones past the last.
 constexpr int kMaskWords = 2 * kMaxWords + 5;
 template <int COLS>
-__device__ __forceinline__ void stage_masks(const TreeArgs& a, const Piece& p, uint32_t (*rows)[kMaskWords]) {
-  const int tok0 = p.c0 / a.group, n_rows = (min(p.c0 + COLS, p.q.n * a.group) - 1) / a.group - tok0 + 1;
-  const int mw = 2 * a.words + 5;
-  for (int i = threadIdx.x; i < n_rows * mw; i += blockDim.x) {
-    const int r = i / mw, k = i - r * mw - 2;
-    uint32_t x = k < 0 ? ~0u : 0u;
-    if (k >= 0 && 32 * k < p.q.n) {
-      x = a.mask[(size_t)(p.q.r0 + tok0 + r) * 2 * a.words + k];
-      if (p.q.n < 32 * k + 32) x &= (1u << (p.q.n - 32 * k)) - 1;
-    }
-    rows[r][k + 2] = x;
+struct Masks {
+  int words, count;  // words of a row; of all rows
+  __device__ __forceinline__ Masks(const TreeArgs& a, const Piece& p) {
+    const int tok0 = p.c0 / a.group, n_rows = (min(p.c0 + COLS, p.q.n * a.group) - 1) / a.group - tok0 + 1;
+    words = 2 * a.words + 5;
+    count = n_rows * words;
   }
-}
+  __device__ __forceinline__ uint32_t value(const TreeArgs& a, const Piece& p, int i) const {
+    const int r = i / words, k = i - r * words - 2;
+    if (k < 0) return ~0u;
+    if (32 * k >= p.q.n) return 0;
+    const uint32_t x = a.mask[(size_t)(p.q.r0 + p.c0 / a.group + r) * 2 * a.words + k];
+    return p.q.n < 32 * k + 32 ? x & ((1u << (p.q.n - 32 * k)) - 1) : x;
+  }
+};
 
 // ---- one wave's columns
 template <int NC>
@@ -410,9 +434,7 @@ __device__ __forceinline__ void note_start(const TreeArgs& a, const Piece& p, in
   a.desc[wg] = d;
 }
 
-// ---- many columns: bound by the matrix cores
-//
-// NW waves of 16 NC columns share every tile through LDS.
+// ---- NW waves of 16 NC columns share every tile through LDS
 template <bool FP8, int NW, int NC>
 __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs a) {
   constexpr int kThreads = NW * 64;
@@ -554,9 +576,9 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs a) {
     }
     st.load_q(a, p, p.c0 + WCOLS * w);
     active = p.c0 + WCOLS * w < p.q.n * a.group;
-    more = walk.next(nxt);
-    if (more) first = block_of(nxt, nxt.j0 + lane);
     later = block_of(p, base + kChunk + lane);
+    const Masks<COLS> masks(a, p);
+    const uint32_t mask0 = tid < masks.count ? masks.value(a, p, tid) : 0;
     cmul = a.scale_log2;
     vsc = 1.0f;
     if constexpr (FP8) {
@@ -564,7 +586,11 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs a) {
       if (cmul == 0.f) cmul = 1e-37f;  // (0 times the -inf of a hidden token is not -inf)
       vsc = a.v_scale[p.g];
     }
-    stage_masks<COLS>(a, p, rows);
+    // the next piece is looked up while all that is on its way
+    more = walk.next(nxt);
+    if (more) first = block_of(nxt, nxt.j0 + lane);
+    if (tid < masks.count) rows[tid / masks.words][tid % masks.words] = mask0;
+    for (int i = tid + kThreads; i < masks.count; i += kThreads) rows[i / masks.words][i % masks.words] = masks.value(a, p, i);
     st.clear();
     if (!linked) {
       if (p.j0 >= (p.q.T - p.q.n) / KT) clean(p.q, p.j0, rA, turn);
@@ -754,6 +780,13 @@ Plan plan(const dp_tree_shape* sh) {
   const int64_t group = sh->n_q_heads / sh->n_kv_heads;
   const int64_t per_seq = (sh->total_q * group + std::max(sh->batch, 1) - 1) / std::max(sh->batch, 1);
   const int cus = compute_units();
+  // Columns of an item follow the average tree (the host does not know the
+  // trees): fewer than a tree has read its cache again for the rest, more leave
+  // waves idle.  us with 64 / 128 / 256: 64 columns a tree (short pool, bf16) 186
+  // / 192 / 198; 16 to 208 (short pool, e4m3, 112 on average) 170 / 155 / 173; 256
+  // (long pool, bf16) 900 / 530 / 440.  Two workgroups of four waves to a compute
+  // unit fill each other's gaps (one: 207 for 186, 213 for 162); eight waves of 32
+  // columns leave registers for one.
   if (per_seq <= 64) return Plan{0, 64, 2 * cus};
   if (per_seq <= 128) return Plan{1, 128, 2 * cus};
   return Plan{2, 256, cus};
