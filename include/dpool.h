@@ -574,8 +574,9 @@ int qk_norm_rope_append(const void* q, const void* k, const void* v, const void*
 /*   tree_mask[r][j / 64] is set                                             */
 /* with K_t, V_t gathered exactly as for paged_decode_attention.  Any bits  */
 /* are allowed: a chain of drafts (bits 0..i), windows, rows that see no    */
-/* draft.  A row that sees no token at all gives zeros.  A cached value of   */
-/* a token that a row does not see never reaches it, finite or not.          */
+/* draft.  A row that sees no token at all, or whose scores are all          */
+/* -infinity, gives zeros.  A cached value of a token that a row does not    */
+/* see never reaches it, finite or not.                                      */
 /*                                                                           */
 /* Layouts: q, out [total_q, n_q_heads, 128] bf16, rows packed as q_start   */
 /* says; tree_mask [total_q, mask_words] 64-bit words, 8-byte aligned; the  */

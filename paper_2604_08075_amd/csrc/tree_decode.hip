@@ -600,6 +600,15 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs a) {
     // Block ids are waited for here, once (the masks' loads behind them were
     // already): else the compiler would wait for all loads in every step.
     __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0)
+    if constexpr (FP8) {
+      if (cmul < 0.f) {  // a scale below 0: the queries change sign instead (-inf hides a token, the largest score leads)
+        cmul = -cmul;
+#pragma unroll
+        for (int b = 0; b < NC; ++b)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) st.qf[b][c] ^= (int)0x80008000;
+      }
+    }
     lds_barrier();
     if (tid == 0) odd[turn ^ 1] = 0;  // (every wave has left the piece before)
   };

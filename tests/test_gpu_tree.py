@@ -253,3 +253,18 @@ def test_committed_values_that_are_not_finite(gpu_lib, T, n, t, fmt):
     hit = np.zeros(got.shape, bool)
     hit[n:, :2, 5:7] = True
     assert np.isnan(got[hit]).all() and np.array_equal(got[~hit], clean[~hit])
+
+
+def test_key_scale_below_zero(gpu_lib):
+    """The formula holds for any scale: hidden tokens stay hidden under a negative one."""
+    note("tree, e4m3 with key scales below 0")
+    chunks = [(3, 50), (4, 4), (9, 700)]
+    w = workloads.make_prefill(chunks, 4, 2, c_max=704, kv_format="fp8_e4m3", seed=52)
+    w.k_scale = w.k_scale * np.float32([-1, -0.5])
+    w.v_scale = w.v_scale * np.float32([1, -2])
+    mask = tree_masks(np.random.default_rng(2), [3, 4, 9], 1, "tree")
+    mask[4] = 0
+    got = call(gpu_lib, w, workloads.to_device(w), mask, 1)
+    ref, bound = tree.tree_attention(w.q_bits, w.k_store.dense(), w.v_store.dense(), w.block_tables, w.context_lens,
+                                     w.meta["q_start"], mask, w.scale, "fp8_e4m3", w.k_scale, w.v_scale)
+    assert (np.abs(got - ref) <= bound).all()
