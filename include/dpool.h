@@ -477,9 +477,9 @@ int chunked_prefill_attention(const void* q, const void* k_blocks, const void* v
 /*   max_blocks_per_seq] int32 (updated in place; entries from the owned    */
 /*   count on are of no meaning); q_start [batch + 1] int32; slots           */
 /*   [total_rows] int64; positions, parents [total_rows] int32.              */
-/* The outputs context_lens_out, n_owned_out, free_state_out and q_start    */
-/* must not be the inputs (DP_EINVAL).  The updates in place leave what the */
-/* call reads alone, so a call repeated on the same inputs does the same.   */
+/* No output may be an input or another output (DP_EINVAL).  The updates in */
+/* place leave what the call reads alone, so a call repeated on the same    */
+/* inputs does the same.                                                     */
 /* One launch; nothing is allocated.  batch <= 4096, block_size 16,         */
 /* total_rows and num_blocks <= 2^30, mask_words 0 (no parents) to 4.       */
 /* DP_EINVAL / DP_ENOTSUP for bad arguments (nothing enqueued), DP_EIO if   */
@@ -637,11 +637,12 @@ int tree_decode_attention(const void* q, const void* k_blocks, const void* v_blo
 /* moved.                                                                    */
 /*   k_layers, v_layers  host arrays of n_layers device pointers, caches as */
 /*                       for kv_cache_append, all of one shape, no two the  */
-/*                       same; read during the call only                     */
+/*                       same (DP_EINVAL); read during the call only         */
 /*   accepted [batch, max_accept] int32, n_accepted [batch] int32;          */
 /*   context_lens_out [batch] int32, not context_lens itself                 */
 /*   shape  mask_words is not looked at                                      */
-/* One launch per 64 layers (n_layers >= 1); nothing is allocated.          */
+/* Blocks that hold drafts belong to one sequence (else the moves race).    */
+/* One launch per 64 layers (n_layers 1 to 1024); nothing is allocated.     */
 /* DP_EINVAL / DP_ENOTSUP for bad arguments (nothing enqueued), DP_EIO if a */
 /* launch fails.                                                             */
 /* ------------------------------------------------------------------------ */

@@ -476,6 +476,8 @@ class CacheLayers:
 def kv_cache_accept(layers: CacheLayers, block_tables, context_lens, q_start, accepted, n_accepted, context_lens_out,
                     shape: TreeShape, stream=None) -> None:
     """Enqueue the move of the accepted drafts, accepted [batch, max_accept] (include/dpool.h, kv_cache_accept)."""
+    if accepted.dim() != 2 or not accepted.is_contiguous():
+        raise ValueError("accepted must be a contiguous [batch, max_accept] tensor")
     check(lib().kv_cache_accept(
         layers.k, layers.v, layers.n, block_tables.data_ptr(), context_lens.data_ptr(), q_start.data_ptr(),
         accepted.data_ptr(), n_accepted.data_ptr(), accepted.shape[1], context_lens_out.data_ptr(),

