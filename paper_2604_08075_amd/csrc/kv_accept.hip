@@ -3,20 +3,19 @@
 // the caches of up to 64 layers per launch.
 //
 // What bounds it: for a step's handful of tokens, latency; one wave takes one
-// (layer, sequence, KV head), so that all moves are in flight together.  For
-// many, the V tiles: a token's V is one column of a dims-major tile, 128
-// values that lie 32 (bf16) or 16 (e4m3) bytes apart, so moving 256 bytes
-// touches a whole 4 KB tile twice.  Measured: paths of up to eight of sixteen
-// drafts, 128 sequences, 16 layers, 8 heads, bf16 (56 MB of values; the memory
-// lines that hold them are 193 MB): 60 us, 3.2 TB/s of those lines; paths of up
-// to five, five sequences, 6 layers, 4 heads, e4m3: 4.4 us.  A lane has dims
-// lane and lane + 64, so that a wave's values lie in fewer lines than with
-// neighbouring pairs, and eight moves in flight instead of four: 77 us before.
+// (layer, sequence, KV head).  For many, the V tiles: a token's V is one column
+// of a dims-major tile, 128 values that lie 32 (bf16) or 16 (e4m3) bytes apart,
+// so moving 256 bytes touches a whole 4 KB tile twice.  So tiles are read and
+// written whole, in 16-byte pieces: a lane holds all tokens of dimensions lane
+// and lane + 64, and a moved value passes from one word of its registers to
+// another.  Measured: paths of up to eight of sixteen drafts, 128 sequences, 16
+// layers, 8 heads, bf16 (56 MB of values, about 210 MB of tiles and rows): 45
+// us, 4.7 TB/s of the latter, a large copy's rate; value by value it was 60.
+// Paths of up to five, five sequences, 6 layers, 4 heads, e4m3: 4.7 us.
 //
 // Entries are strictly increasing, accepted[j] >= j, and only one wave works
-// on a tile.  A group of moves reads all its sources before it writes; what a
-// later group reads lies at or behind its own targets, which no earlier group
-// has written.
+// on a tile.  A target block's moves are read before it is written, and a later
+// block's sources lie at or behind it, which nothing has written.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -27,13 +26,14 @@
 
 namespace dpool_accept {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kD = 128;
 constexpr int kBS = 16;
 constexpr int kWaves = 4;
 constexpr int kMaxLayers = 64;  // per launch: their addresses are kernel arguments
 constexpr int kMaxBatch = 4096;
 constexpr int kMaxCall = 1024;  // layers of a call
-constexpr int kMoves = 8;       // moves in flight together
 
 struct AcceptArgs {
   char* k[kMaxLayers];
@@ -53,6 +53,10 @@ template <bool FP8>
 __global__ __launch_bounds__(kWaves * 64) void kv_accept_kernel(AcceptArgs a) {
   using Code = std::conditional_t<FP8, uint8_t, uint16_t>;
   using Pair = std::conditional_t<FP8, uint16_t, uint32_t>;
+  constexpr int kRegs = FP8 ? 1 : 2;  // 16-byte pieces of a dimension's tokens
+  constexpr int N = FP8 ? 4 : 2, BITS = 32 / N;  // tokens of a word
+  constexpr uint32_t ONES = (1u << BITS) - 1;
+  typedef i32x4 Tile[2][kRegs];  // dimensions lane and lane + 64 of a V tile
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
   if (unit >= a.units) return;
@@ -68,6 +72,13 @@ __global__ __launch_bounds__(kWaves * 64) void kv_accept_kernel(AcceptArgs a) {
   Code* const vl = (Code*)a.v[layer];
   const int32_t* const bt = a.tables + (size_t)s * a.max_blocks;
 
+  const auto load = [&](const Code* p, Tile& x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < kRegs; ++i) x[h][i] = ((const i32x4*)(p + (lane + 64 * h) * kBS))[i];
+  };
+
   int last = -1, done = 0;  // the last entry so far, and how many were valid
   for (int j0 = 0; j0 < want; j0 += 64) {
     const int j = j0 + lane;
@@ -76,46 +87,66 @@ __global__ __launch_bounds__(kWaves * 64) void kv_accept_kernel(AcceptArgs a) {
     if (lane == 0) prev = last;
     const uint64_t bad = __ballot(idx <= prev || idx >= n);  // (idx >= 0 follows from idx > prev >= -1)
     const int ok = bad ? __builtin_ctzll(bad) : 64;
-    // tile rows (block, slot) of this lane's move
-    int64_t src = -1, dst = -1;
+    // this lane's move: block and slot that it reads, those that it writes, and their places in the table
+    int from = -1, to = -1, s_from = 0, s_to = 0, p_from = -1, p_to = -1;
     if (lane < ok && idx != j) {
       const int ts = T - n + idx, td = T - n + j;
-      const int bs = bt[ts / kBS], bd = bt[td / kBS];
-      if (bs >= 0 && bs < a.num_blocks && bd >= 0 && bd < a.num_blocks) {
-        src = (int64_t)bs * kBS + ts % kBS;
-        dst = (int64_t)bd * kBS + td % kBS;
+      from = bt[ts / kBS], to = bt[td / kBS];
+      if (from >= 0 && from < a.num_blocks && to >= 0 && to < a.num_blocks) {
+        p_from = ts / kBS, s_from = ts % kBS;
+        p_to = td / kBS, s_to = td % kBS;
       }
     }
-    uint64_t todo = __ballot(src >= 0);
+    uint64_t todo = __ballot(p_to >= 0);
     while (todo) {
-      Pair kv[kMoves];
-      Code v0[kMoves], v1[kMoves];
-      int64_t to[kMoves];
+      // the moves into one block: consecutive lanes, consecutive slots
+      const int f = __builtin_ctzll(todo), first = __builtin_amdgcn_readlane(s_to, f) - f;  // slot of lane 0
+      const uint64_t mine = __ballot(p_to == __builtin_amdgcn_readlane(p_to, f));
+      todo &= ~mine;
+      uint32_t left = (uint32_t)(mine >> f) << (first + f);  // by slot
+      const size_t tile = ((size_t)__builtin_amdgcn_readlane(to, f) * a.hkv + g) * (kBS * kD);
+      Tile d, x;
+      load(vl + tile, d);
+      Pair k[kBS];
 #pragma unroll
-      for (int i = 0; i < kMoves; ++i) {
-        to[i] = -1;
-        if (todo) {  // (the same for every lane)
-          const int f = __builtin_ctzll(todo);
-          todo &= todo - 1;
-          const int64_t from = __shfl(src, f);
-          to[i] = __shfl(dst, f);
-          const size_t tile = ((size_t)(from / kBS) * a.hkv + g) * (kBS * kD);
-          const int slot = (int)(from % kBS);
-          kv[i] = *(const Pair*)(kl + tile + slot * kD + 2 * lane);
-          v0[i] = vl[tile + lane * kBS + slot];
-          v1[i] = vl[tile + (lane + 64) * kBS + slot];
+      for (int t = 0; t < kBS; ++t)
+        if (left >> t & 1) {
+          const size_t at = ((size_t)__builtin_amdgcn_readlane(from, t - first) * a.hkv + g) * kBS;
+          k[t] = *(const Pair*)(kl + (at + __builtin_amdgcn_readlane(s_from, t - first)) * kD + 2 * lane);
         }
+#pragma unroll
+      for (int t = 0; t < kBS; ++t)
+        if (left >> t & 1) *(Pair*)(kl + tile + t * kD + 2 * lane) = k[t];
+      while (left) {
+        // those that come from one block
+        const int e = __builtin_ctz(left) - first, p = __builtin_amdgcn_readlane(p_from, e);
+        const uint32_t here = (uint32_t)((__ballot(p_from == p) & mine) >> f) << (first + f);
+        left &= ~here;
+        if (p == __builtin_amdgcn_readlane(p_to, f)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < kRegs; ++i) x[h][i] = d[h][i];
+        } else load(vl + ((size_t)__builtin_amdgcn_readlane(from, e) * a.hkv + g) * (kBS * kD), x);
+#pragma unroll
+        for (int t = 0; t < kBS; ++t)
+          if (here >> t & 1) {
+            const int s0 = __builtin_amdgcn_readlane(s_from, t - first);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t w = (uint32_t)x[h][0][0];
+#pragma unroll
+              for (int i = 1; i < 4 * kRegs; ++i) w = s0 / N == i ? (uint32_t)x[h][i / 4][i % 4] : w;
+              const uint32_t code = w >> (s0 % N * BITS) & ONES;
+              const uint32_t rest = (uint32_t)d[h][t / N / 4][t / N % 4] & ~(ONES << (t % N * BITS));
+              d[h][t / N / 4][t / N % 4] = (int)(rest | code << (t % N * BITS));
+            }
+          }
       }
 #pragma unroll
-      for (int i = 0; i < kMoves; ++i) {
-        if (to[i] >= 0) {
-          const size_t tile = ((size_t)(to[i] / kBS) * a.hkv + g) * (kBS * kD);
-          const int slot = (int)(to[i] % kBS);
-          *(Pair*)(kl + tile + slot * kD + 2 * lane) = kv[i];
-          vl[tile + lane * kBS + slot] = v0[i];
-          vl[tile + (lane + 64) * kBS + slot] = v1[i];
-        }
-      }
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < kRegs; ++i) ((i32x4*)(vl + tile + (lane + 64 * h) * kBS))[i] = d[h][i];
     }
     done += min(ok, want - j0);
     if (bad && ok < want - j0) break;
@@ -162,8 +193,8 @@ extern "C" int kv_cache_accept(void* const* k_layers, void* const* v_layers, int
     return fail(DP_EINVAL, "kv_cache_accept: pointers must be 4-byte aligned");
   for (int32_t i = 0; i < n_layers; ++i) {
     if (!k_layers[i] || !v_layers[i]) return fail(DP_EINVAL, "kv_cache_accept: null cache of layer %d", i);
-    if (((uintptr_t)k_layers[i] | (uintptr_t)v_layers[i]) & 3)
-      return fail(DP_EINVAL, "kv_cache_accept: caches must be 4-byte aligned");
+    if (((uintptr_t)k_layers[i] | (uintptr_t)v_layers[i]) & 15)
+      return fail(DP_EINVAL, "kv_cache_accept: caches must be 16-byte aligned");
     if (k_layers[i] == v_layers[i])
       return fail(DP_EINVAL, "kv_cache_accept: K and V of layer %d are the same cache", i);
     // (a cache given twice would move its tokens twice, in two waves at once)
