@@ -641,7 +641,8 @@ int tree_decode_attention(const void* q, const void* k_blocks, const void* v_blo
 /*   accepted [batch, max_accept] int32, n_accepted [batch] int32;          */
 /*   context_lens_out [batch] int32, not context_lens itself                 */
 /*   shape  mask_words is not looked at                                      */
-/* Blocks that hold drafts belong to one sequence (else the moves race).    */
+/* Blocks that hold drafts belong to one sequence, and nothing else writes  */
+/* to them meanwhile: their V tiles are written whole.                       */
 /* One launch per 64 layers (n_layers 1 to 1024); nothing is allocated.     */
 /* DP_EINVAL / DP_ENOTSUP for bad arguments (nothing enqueued), DP_EIO if a */
 /* launch fails.                                                             */
