@@ -9,9 +9,9 @@
 // written whole, in 16-byte pieces: a lane holds all tokens of dimensions lane
 // and lane + 64, and a moved value passes from one word of its registers to
 // another.  Measured: paths of up to eight of sixteen drafts, 128 sequences, 16
-// layers, 8 heads, bf16 (56 MB of values, about 210 MB of tiles and rows): 45
-// us, 4.7 TB/s of the latter, a large copy's rate; value by value it was 60.
-// Paths of up to five, five sequences, 6 layers, 4 heads, e4m3: 4.7 us.
+// layers, 8 heads, bf16 (56 MB of values; counted 108 MB read, 81 MB written):
+// 45 us, 4.2 TB/s (a large copy: 4.8); value by value it was 60.  Paths of up to
+// five, five sequences, 6 layers, 4 heads, e4m3: 4.7 us.
 //
 // Entries are strictly increasing, accepted[j] >= j, and only one wave works
 // on a tile.  A target block's moves are read before it is written, and a later
