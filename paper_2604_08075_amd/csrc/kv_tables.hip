@@ -12,8 +12,9 @@
 // workgroup scans the whole batch by itself (the lengths come from L2, a batch
 // of 256 in one go), and then takes its share of the rows: no workgroup waits
 // for another, and there is no second launch.  Measured, per call: 256 single
-// tokens 6.0 us, 96 trees of up to 32 drafts 6.6, 512 prompts of 722,154 tokens
-// (9 MB of slots, positions and tables, 0.7 TB/s) 12.6.
+// tokens 5.8 us, 96 trees of up to 32 drafts 7.2, 512 prompts of 722,154 tokens
+// (9 MB of slots, positions and tables, 0.9 TB/s) 10.4; with ten barriers a scan
+// and wave sums by permutes instead of two and lane shifts 7.0, 7.7 and 12.0.
 // A row's sequence is found by a binary search over the running sums in LDS.
 //
 // Nothing that the call reads is written by it (the ring's tail and the table
@@ -31,7 +32,7 @@ constexpr int kBS = 16;
 constexpr int kMaxBatch = 4096;
 constexpr int kMaxWords = 4;
 constexpr int64_t kMaxCount = (int64_t)1 << 30;  // rows and blocks: two such counts add up in 32 bits
-constexpr int kMaxThreads = 1024;
+constexpr int kMaxThreads = 512;
 
 struct TablesArgs {
   const int32_t* context;
@@ -53,23 +54,34 @@ struct TablesArgs {
   uint32_t rows, blocks;
 };
 
-// Inclusive running sum over the workgroup, cut at `lim` (a, b <= 2^30 + 1
-// each, so that no sum passes 32 bits; cutting at every step equals cutting
-// the whole sum).  `carry` is the sum of the chunks before; wsum one word a wave.
-__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t lim, uint32_t carry, uint32_t* wsum) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+// Inclusive running sum over a wave, cut at `lim` (a, b <= 2^30 + 1 each, so
+// that no sum passes 32 bits; cutting at every step equals cutting the whole
+// sum); the wave's last one goes to wsum.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t add_lanes(uint32_t x, uint32_t lim) {
+  return min(x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, true), lim);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, uint32_t lim, uint32_t* wsum) {
   x = min(x, lim);
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint32_t y = __shfl_up(x, off);
-    if (lane >= off) x = min(x + y, lim);
+  x = add_lanes<0x111, 0xf>(x, lim);  // from 1, 2, 4 and 8 lanes before, within rows of sixteen
+  x = add_lanes<0x112, 0xf>(x, lim);
+  x = add_lanes<0x114, 0xf>(x, lim);
+  x = add_lanes<0x118, 0xf>(x, lim);
+  x = add_lanes<0x142, 0xa>(x, lim);  // the end of row 0 to row 1, of 2 to 3
+  x = add_lanes<0x143, 0xc>(x, lim);  // the end of row 1 to rows 2 and 3
+  if ((threadIdx.x & 63) == 63) wsum[threadIdx.x >> 6] = x;
+  return x;
+}
+
+// The same over the workgroup, once all waves' sums are there.  `carry`: the sum of the chunks before, then of this too.
+__device__ __forceinline__ uint32_t join_waves(uint32_t x, uint32_t lim, const uint32_t* wsum, uint32_t& carry) {
+  const int w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  uint32_t before = carry;
+  for (int k = 0; k < nw; ++k) {
+    if (k == w) before = carry;
+    carry = min(carry + wsum[k], lim);
   }
-  if (lane == 63) wsum[w] = x;
-  __syncthreads();
-  for (int k = 0; k < nw; ++k)
-    if (k < w) carry = min(carry + wsum[k], lim);
-  __syncthreads();  // wsum is free again
-  return min(x + carry, lim);
+  return min(x + before, lim);
 }
 
 // Largest s with start[s] <= i (start non-decreasing, start[0] = 0 <= i).
@@ -87,7 +99,7 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
   // [B + 1] first row, [B + 1] first released block, [B] first new block of
   // the ring (~0: refused), [threads] + 256 parents of the rows at hand
   extern __shared__ uint32_t lds[];
-  __shared__ uint32_t wsum[kMaxThreads / 64];
+  __shared__ uint32_t wsum[3][kMaxThreads / 64], took;
   const int B = a.batch, tid = threadIdx.x, nt = blockDim.x;
   uint32_t* const row0 = lds;
   uint32_t* const back0 = row0 + B + 1;
@@ -99,26 +111,30 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
   if (head >= nb) head %= nb;
   const uint32_t free = min((uint32_t)max(a.state_in[1], 0), nb);
 
-  uint32_t rows_c = 0, back_c = 0, need_c = 0, took = 0;  // sums of the chunks before
-  if (tid == 0) row0[0] = back0[0] = 0;
+  uint32_t rows_c = 0, back_c = 0, need_c = 0;  // sums of the chunks before
+  if (tid == 0) row0[0] = back0[0] = took = 0;
+  int x1 = 0, c1 = 0, b1 = 0;  // a chunk ahead
+  if (tid < B) x1 = a.fresh[tid], c1 = a.context[tid], b1 = a.owned[tid];
   for (int base = 0; base < B; base += nt) {
-    const int s = base + tid;
-    int x = 0, c = 0, b = 0;
-    if (s < B) {
-      x = a.fresh[s];
-      c = a.context[s];
-      b = a.owned[s];
-    }
+    const int s = base + tid, x = x1;
+    int c = c1, b = b1;
+    x1 = 0;
+    if (s + nt < B) x1 = a.fresh[s + nt], c1 = a.context[s + nt], b1 = a.owned[s + nt];
     const uint32_t n = (uint32_t)max(x, 0);
     c = (int)min((int64_t)max(c, 0), cap);
     b = min(max(b, 0), a.max_blocks);
-    const uint32_t rows_end = block_scan(n, a.rows + 1, rows_c, wsum);
-    const uint32_t back_end = block_scan(x < 0 ? (uint32_t)b : 0, nb, back_c, wsum);
+    const uint32_t n_upto = wave_scan(n, a.rows + 1, wsum[0]);
+    const uint32_t back_upto = wave_scan(x < 0 ? (uint32_t)b : 0, nb, wsum[1]);
+    __syncthreads();
+    const uint32_t rows_end = join_waves(n_upto, a.rows + 1, wsum[0], rows_c);
+    const uint32_t back_end = join_waves(back_upto, nb, wsum[1], back_c);
     b = max(b, (c + kBS - 1) / kBS);
     const int64_t want = (int64_t)c + n;
     const bool fits = want <= cap && rows_end <= a.rows && !(a.parents && n > 64u * a.words);
     const uint32_t need = fits && x > 0 ? (uint32_t)max((int64_t)0, (want + kBS - 1) / kBS - b) : 0;
-    const uint32_t need_end = block_scan(need, nb + 1, need_c, wsum);
+    const uint32_t need_upto = wave_scan(need, nb + 1, wsum[2]);
+    __syncthreads();  // (what the next chunk writes, everyone has read by then)
+    const uint32_t need_end = join_waves(need_upto, nb + 1, wsum[2], need_c);
     const bool ok = fits && (need == 0 || need_end <= free);
     if (s < B) {
       row0[s + 1] = min(rows_end, a.rows);
@@ -132,34 +148,15 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
       }
     }
     // the last sum that the free ids still cover is what was taken
-    const uint32_t met = ok && need ? need_end : 0;
-    // (the carries: the last thread's sums)
-    if (tid == nt - 1) {
-      wsum[0] = rows_end;
-      wsum[1] = back_end;
-      wsum[2] = need_end;
-    }
-    __syncthreads();
-    rows_c = wsum[0];
-    back_c = wsum[1];
-    need_c = wsum[2];
-    __syncthreads();
-    // largest of `met` over the workgroup (sums grow with s)
-    uint32_t m = met;
-#pragma unroll
-    for (int off = 32; off; off >>= 1) m = max(m, (uint32_t)__shfl_xor(m, off));
-    if ((tid & 63) == 0) wsum[tid >> 6] = m;
-    __syncthreads();
-    for (int k = 0; k < nt >> 6; ++k) took = max(took, wsum[k]);
-    __syncthreads();
+    if (blockIdx.x == 0 && ok && need) atomicMax(&took, need_end);
   }
+  __syncthreads();
   const uint32_t back = min(back_c, nb - free);  // more would overtake the ring's head: ids that were never handed out
   if (blockIdx.x == 0 && tid == 0) {
     a.q_start[0] = 0;
     a.state_out[0] = (int)((head + took) % nb);  // (both below 2^30 + 1)
     a.state_out[1] = (int)(free - took + back);
   }
-  __syncthreads();  // (an empty batch)
   const uint32_t rows_used = row0[B];
 
   // released blocks
@@ -299,12 +296,15 @@ extern "C" int kv_tables_step(const int32_t* context_lens, const int32_t* n_owne
   a.words = sh->mask_words;
   a.rows = (uint32_t)sh->total_rows;
   a.blocks = (uint32_t)sh->num_blocks;
-  const int threads = 256;
-  // One workgroup per 256 rows, or per 4,096 table entries that may have to go
-  // back; up to four on a compute unit (722,154 rows of 512 prompts: 22.0 us with
-  // at most 256 workgroups, 14.3 with 1,024, 20.4 with 2,048, as each scans the
-  // batch).
-  const int64_t groups = std::min<int64_t>(1024, std::max((sh->total_rows + threads - 1) / threads,
+  const int threads = sh->batch > 256 ? 512 : 256;
+  // Threads: the scan takes a batch in as few turns as its size asks for, a small
+  // batch with few waves at each barrier (96 trees: 7.4 us with 256, 7.7 with 512;
+  // 722,154 rows of 512 prompts 14.2 / 10.9; of 2,048 34.7 / 23.7).  Workgroups:
+  // one to as many rows as it has threads, or to 4,096 table entries that may
+  // have to go back, at most what fills half of the device's wave slots, as each
+  // scans the batch (512 prompts: 13.3 us with half as many, 10.4; 15.8 for 12.0
+  // with twice as many, before the scan had two barriers instead of ten).
+  const int64_t groups = std::min<int64_t>((1 << 18) / threads, std::max((sh->total_rows + threads - 1) / threads,
                                                          (int64_t)sh->batch * sh->max_blocks_per_seq / 4096));
   const size_t dyn = (size_t)(3 * sh->batch + 2 + (parents ? threads + 64 * kMaxWords : 0)) * sizeof(uint32_t);
   (void)hipGetLastError();
