@@ -140,3 +140,18 @@ def test_tables_many_steps_on_the_device(gpu_lib):
         assert np.array_equal(b["ctx"].cpu().numpy(), ctx) and np.array_equal(b["owned"].cpu().numpy(), owned)
         assert np.array_equal(dring.cpu().numpy(), ring) and np.array_equal(dtb.cpu().numpy(), tb)
         assert b["st"].tolist() == [head, count] and np.array_equal(o["slots"].cpu().numpy(), w["slots"])
+
+
+def test_tables_trees_of_a_large_batch(gpu_lib):
+    """More sequences than one turn of the scan takes, with trees, refusals and sequences that end."""
+    note("tables with trees, 1100 sequences")
+    rng = np.random.default_rng(77)
+    B, mb = 1100, 6
+    ctx, owned, tb, ring, head = state(rng, B, mb, 500)
+    new = rng.integers(-1, 20, B)
+    new[[3, 600, 1099]] = 65                   # larger than the masks: refused
+    rows = int(np.maximum(new, 0).sum())
+    par = np.concatenate([rng.integers(-1, np.maximum(np.arange(max(n, 0)), 1), max(n, 0)) for n in new])
+    want = tables.step(ctx, owned, new, ring, head, 500, tb, rows, par, 1)
+    assert 0 < want["granted"].sum() < B
+    same(run(gpu_lib, ctx, owned, new, ring, head, 500, tb, rows, par, 1), want)
