@@ -531,7 +531,7 @@ int kv_tables_step(const int32_t* context_lens, const int32_t* n_owned, const in
 /*   cos_sin [n_positions, rotary_dim] fp32; positions [rows] int32;         */
 /*   slots [rows] int64                                                      */
 /*   q_out [rows, n_q_heads, 128] bf16, contiguous; may be q itself where    */
-/*   q_stride is n_q_heads * 128                                             */
+/*   q_stride is n_q_heads * 128, and overlaps none of the inputs otherwise  */
 /*   k_blocks, v_blocks, k_scale, v_scale: as for kv_cache_append            */
 /* q, k, v, weights, cos_sin, q_out and the caches are 16-byte aligned.     */
 /* rotary_dim is a multiple of 16 in [0, 128].  One launch; nothing is      */
@@ -586,7 +586,8 @@ int qk_norm_rope_append(const void* q, const void* k, const void* v, const void*
 /* Probabilities enter the second product as bf16 (the denominator sums the */
 /* rounded ones); everything else is fp32 until out is rounded.              */
 /*   workspace >= tree_decode_workspace_size(shape) bytes, 256-byte aligned, */
-/* of any content; calls that share one must not overlap in time.           */
+/*   of any content; calls that share one must not overlap in time.  q, out  */
+/*   and workspace do not overlap (DP_EINVAL where they start together).      */
 /* Results are deterministic.  At most two launches; nothing is allocated.  */
 /* Supported: head_dim 128, block_size 16, Hq a multiple of Hkv,            */
 /* batch <= 4096, mask_words 1..4, Hq / Hkv <= 1024.                        */
@@ -639,7 +640,7 @@ int tree_decode_attention(const void* q, const void* k_blocks, const void* v_blo
 /*                       for kv_cache_append, all of one shape, no two the  */
 /*                       same (DP_EINVAL); read during the call only         */
 /*   accepted [batch, max_accept] int32, n_accepted [batch] int32;          */
-/*   context_lens_out [batch] int32, not context_lens itself                 */
+/*   context_lens_out [batch] int32, none of the inputs (DP_EINVAL)          */
 /*   shape  mask_words is not looked at                                      */
 /* Blocks that hold drafts belong to one sequence, and nothing else writes  */
 /* to them meanwhile: their V tiles are written whole.                       */

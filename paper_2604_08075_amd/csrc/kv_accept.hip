@@ -186,7 +186,8 @@ extern "C" int kv_cache_accept(void* const* k_layers, void* const* v_layers, int
   if (!k_layers || !v_layers || !block_tables || !context_lens || !q_start || !accepted || !n_accepted ||
       !context_lens_out)
     return fail(DP_EINVAL, "kv_cache_accept: null pointer");
-  if (context_lens_out == context_lens || context_lens_out == n_accepted || context_lens_out == q_start)
+  if (context_lens_out == context_lens || context_lens_out == n_accepted || context_lens_out == q_start ||
+      context_lens_out == accepted || context_lens_out == block_tables)
     return fail(DP_EINVAL, "kv_cache_accept: context_lens_out must not be an input");
   if (((uintptr_t)block_tables | (uintptr_t)context_lens | (uintptr_t)q_start | (uintptr_t)accepted |
        (uintptr_t)n_accepted | (uintptr_t)context_lens_out) & 3)

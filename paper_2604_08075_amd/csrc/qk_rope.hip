@@ -368,6 +368,7 @@ extern "C" int qk_norm_rope_append(const void* q, const void* k, const void* v, 
     return fail(DP_EINVAL, "qk_norm_rope_append: positions, slots and scales must be aligned to their elements");
   if (q_out == q && sh->q_stride != (int64_t)sh->n_q_heads * kD)
     return fail(DP_EINVAL, "qk_norm_rope_append: q_out may be q only where q_stride is n_q_heads * 128");
+  if (q_out == k || q_out == v) return fail(DP_EINVAL, "qk_norm_rope_append: q_out must not be k or v");
   if ((q_weight || k_weight) && !(eps >= 0.0f && std::isfinite(eps)))
     return fail(DP_EINVAL, "qk_norm_rope_append: eps must be finite and >= 0");
 

@@ -850,6 +850,9 @@ extern "C" int tree_decode_attention(const void* q, const void* k_blocks, const 
     return fail(DP_EINVAL, "tree_decode_attention: workspace must be 256-byte aligned");
   if (workspace_bytes < need)
     return fail(DP_ENOMEM, "tree_decode_attention: workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  // (several workgroups read a row of q, and the first may have written its results)
+  if (out == q || workspace == q || workspace == out)
+    return fail(DP_EINVAL, "tree_decode_attention: q, out and workspace must not be one another");
 
   TreeArgs a;
   a.q = (const uint16_t*)q;

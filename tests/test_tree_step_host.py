@@ -187,3 +187,14 @@ def test_binding_refuses_a_sliced_path(host_lib):
     for accepted in (x[:, :3], x[0]):
         with pytest.raises(ValueError):
             host_lib.kv_cache_accept(layers, x, x, x, accepted, x, x, tshape(host_lib))
+
+
+def test_outputs_that_are_inputs_refused(host_lib):
+    L, s = host_lib.lib(), tshape(host_lib)
+    rest = [P + 4096 * i for i in range(1, 7)]
+    for q, out, ws in ((P, P, 32 * P), (P, 32 * P, P), (P, 32 * P, 32 * P)):
+        assert L.tree_decode_attention(q, *rest, 1.0, None, None, out, ctypes.byref(s), ws, 1 << 30, None) == EINVAL
+    for name in ("tables", "ctx", "q_start", "accepted", "n_accepted"):
+        assert accept(host_lib, out=9 * P, **{name: 9 * P}) == EINVAL
+    for name in ("k", "v"):
+        assert qk(host_lib, {name: 2 * P}) == EINVAL and "q_out" in host_lib.last_error()
