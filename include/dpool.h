@@ -582,7 +582,9 @@ int qk_norm_rope_append(const void* q, const void* k, const void* v, const void*
 /* says; tree_mask [total_q, mask_words] 64-bit words, 8-byte aligned; the  */
 /* rest as for chunked_prefill_attention.  A caller promise: n <= T and     */
 /* n <= 64 * mask_words.  Values that break it are clamped: no access        */
-/* leaves the buffers, rows past the clamped n are left unwritten.           */
+/* leaves the buffers, rows past the clamped n are left unwritten.  An       */
+/* offset of q_start below one before it counts as the largest so far, so    */
+/* that no row belongs to two sequences.                                      */
 /* Probabilities enter the second product as bf16 (the denominator sums the */
 /* rounded ones); everything else is fp32 until out is rounded.              */
 /*   workspace >= tree_decode_workspace_size(shape) bytes, 256-byte aligned, */

@@ -138,15 +138,18 @@ __device__ __forceinline__ ConstInts constants(const int32_t* p) { return (Const
 // What an item needs to know of its sequence
 struct Seq {
   int r0, n, T;
+  int r1;  // the first row of the next sequence
 };
 
-__device__ __forceinline__ Seq sequence(const TreeArgs& a, int s) {
+// Sequence s, whose rows start at r0, where those of the sequence before end:
+// offsets out of order count as the largest so far, so that no row has two
+// sequences, whose workgroups would both write it.
+__device__ __forceinline__ Seq sequence(const TreeArgs& a, int s, int r0) {
   Seq q;
-  const ConstInts start = constants(a.q_start);
-  q.r0 = min(max(start[s], 0), a.total_q);
-  const int r1 = min(max(start[s + 1], q.r0), a.total_q);
+  q.r0 = r0;
+  q.r1 = min(max(constants(a.q_start)[s + 1], r0), a.total_q);
   q.T = min(max(constants(a.context_lens)[s], 0), a.max_ctx);
-  q.n = min(min(r1 - q.r0, q.T), 64 * a.words);
+  q.n = min(min(q.r1 - r0, q.T), 64 * a.words);
   return q;
 }
 
@@ -174,7 +177,7 @@ template <int COLS, int KT>
 struct Walk {
   const TreeArgs& a;
   uint64_t u, u_hi, at, slice;  // next unit, end of the slice, first unit of sequence s
-  int s, wg;
+  int s, row, wg;               // row: the first of sequence s
 
   __device__ __forceinline__ uint32_t units(const Seq& q) const { return (uint32_t)((q.T + KT - 1) / KT + kItemCost); }
   __device__ __forceinline__ uint32_t items(const Seq& q) const {
@@ -186,26 +189,49 @@ struct Walk {
   template <int kThreads>
   __device__ __forceinline__ void begin() {
     __shared__ uint64_t sums[kThreads / 64];
+    __shared__ int mixed[kThreads / 64];
     __shared__ uint64_t found_at;
-    __shared__ int found;
+    __shared__ int found, found_row;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, nwg = gridDim.x;
     // consecutive slices on one XCD (workgroups go to the eight in turn)
     wg = nwg % 8 == 0 ? (int)(blockIdx.x % 8) * (nwg / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
     const int per_thread = (a.batch + kThreads - 1) / kThreads;
     const int s_lo = min(tid * per_thread, a.batch), s_hi = min(s_lo + per_thread, a.batch);
-    uint64_t mine = 0;
-    for (int i = s_lo; i < s_hi; ++i) {
-      const Seq q = sequence(a, i);
-      mine += (uint64_t)units(q) * items(q);
-    }
-    uint64_t upto = mine;
+    const ConstInts start = constants(a.q_start);
+    int row_lo = min(max(start[s_lo], 0), a.total_q);
+    uint64_t mine, upto;
+    for (bool again = false;; again = true) {
+      mine = 0;
+      int r = row_lo;
+      bool disorder = false;
+      for (int i = s_lo; i < s_hi; ++i) {
+        const Seq q = sequence(a, i, r);
+        mine += (uint64_t)units(q) * items(q);
+        disorder |= start[i] > start[i + 1];
+        r = q.r1;
+      }
+      upto = mine;
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const uint64_t y = __shfl_up(upto, off);
-      if (lane >= off) upto += y;
+      for (int off = 1; off < 64; off <<= 1) {
+        const uint64_t y = __shfl_up(upto, off);
+        if (lane >= off) upto += y;
+      }
+      const bool any = __builtin_amdgcn_ballot_w64(disorder) != 0;
+      if (lane == 63) {
+        sums[w] = upto;
+        mixed[w] = any;
+      }
+      __syncthreads();
+      bool all_mixed = false;
+#pragma unroll
+      for (int k = 0; k < kThreads / 64; ++k) all_mixed |= mixed[k] != 0;
+      if (again || !all_mixed) break;
+      // offsets out of order, a broken promise: the largest so far, slowly
+      int most = 0;
+      for (int i = 0; i <= s_lo; ++i) most = max(most, start[i]);
+      row_lo = min(most, a.total_q);
+      __syncthreads();  // (sums and mixed are written again)
     }
-    if (lane == 63) sums[w] = upto;
-    __syncthreads();
     uint64_t total = 0, before = 0;
 #pragma unroll
     for (int k = 0; k < kThreads / 64; ++k) {
@@ -218,32 +244,37 @@ struct Walk {
     upto += before;
     if (u < u_hi && mine > 0 && upto - mine <= u && u < upto) {
       uint64_t x = upto - mine;
+      int r = row_lo;
       for (int i = s_lo; i < s_hi; ++i) {
-        const Seq q = sequence(a, i);
+        const Seq q = sequence(a, i, r);
         const uint64_t y = (uint64_t)units(q) * items(q);
         if (u < x + y) {
           found = i;
           found_at = x;
+          found_row = r;
           break;
         }
         x += y;
+        r = q.r1;
       }
     }
     __syncthreads();
     if (u < u_hi) {
       s = uniform(found);
       at = uniform(found_at);
+      row = uniform(found_row);
     }
   }
 
   // The next piece of the slice that holds a tile; false: there is none.
   __device__ __forceinline__ bool next(Piece& p) {
     while (u < u_hi) {
-      const Seq q = sequence(a, s);
+      const Seq q = sequence(a, s, row);
       const uint32_t iu = units(q);
       const uint64_t end = at + (uint64_t)iu * items(q);
       if (u >= end) {
         at = end;
+        row = q.r1;
         ++s;
         continue;
       }
@@ -700,7 +731,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int cols) {
   const Sums s0 = read(2 * wg + 1), s1 = read(2 * next);
   const TreePiece d = a.desc[wg];
   if (d.last < 0) return;
-  const Seq q{d.r0, d.n, d.T};
+  const Seq q{d.r0, d.n, d.T, d.r0 + d.n};
   const int cc = d.c0 + col;
   if (cc >= q.n * a.group) return;
   const float vsc = FP8 ? a.v_scale[d.g] : 1.0f;

@@ -268,3 +268,30 @@ def test_key_scale_below_zero(gpu_lib):
     ref, bound = tree.tree_attention(w.q_bits, w.k_store.dense(), w.v_store.dense(), w.block_tables, w.context_lens,
                                      w.meta["q_start"], mask, w.scale, "fp8_e4m3", w.k_scale, w.v_scale)
     assert (np.abs(got - ref) <= bound).all()
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("B", [7, 300, 1200])
+def test_row_offsets_out_of_order(gpu_lib, B, fmt):
+    """Offsets below one before them count as the largest so far: the same bits as with those, and no row has two owners."""
+    note(f"tree, row offsets out of order, B={B} {fmt}")
+    rng = np.random.default_rng(B)
+    chunks = [(int(rng.integers(0, 4)), int(rng.integers(3, 40))) for _ in range(B)]
+    w = workloads.make_prefill(chunks, 2, 1, c_max=48, kv_format=fmt, seed=B)
+    qs = np.asarray(w.meta["q_start"], np.int64)
+    total = int(qs[-1])
+    bad = qs.copy()
+    at = rng.choice(B - 1, 3 + B // 50, replace=False) + 1
+    bad[at] = rng.integers(-5, total + 1, len(at))
+    bad[B // 2], bad[0] = -2 ** 31, min(2, total)
+    bad[B - 1] = 2 ** 31 - 1 if B > 500 else bad[B - 1]
+    ordered = np.minimum(np.maximum.accumulate(np.maximum(bad, 0)), total)
+    assert (np.diff(bad) < 0).any() and (ordered != qs).any()
+    mask = tree_masks(rng, [total], 1, "any")
+    d = workloads.to_device(w)
+    got = call(gpu_lib, w, d, mask, 1, q_start=bad, total_q=total)
+    want = call(gpu_lib, w, d, mask, 1, q_start=ordered, total_q=total)
+    assert np.array_equal(got, want, equal_nan=True)
+    n = np.diff(ordered)
+    # (at most as many rows as a sequence has tokens)
+    assert np.isfinite(want).any() and np.isnan(want).all((1, 2)).sum() == total - np.minimum(n, [t for _, t in chunks]).sum()
