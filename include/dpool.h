@@ -460,7 +460,8 @@ int chunked_prefill_attention(const void* q, const void* k_blocks, const void* v
 /* The rows of a refused sequence have no tokens in the cache: attention's   */
 /* results for them are of no use.                                           */
 /* Row i of s is cached at t = c + i:                                        */
-/*     slots = block_tables[s][t / 16] * 16 + t % 16 (-1 if not granted)     */
+/*     slots = block_tables[s][t / 16] * 16 + t % 16 (-1 if not granted, or  */
+/*     where that entry is below 0)                                           */
 /*     positions = t, or with parents c + (number of ancestors)              */
 /* Rows behind the last sequence (a batch padded to a fixed size) get slot  */
 /* -1, position -1 and an empty mask.                                        */

@@ -36,7 +36,8 @@ def step(ctx, owned, new, ring, head, count, tables, total_rows, parents=None, w
                mask=np.zeros((total_rows, max(words, 1)), np.uint64))
     want_so_far = took = gave = rows = 0
     for s in range(B):
-        c, b, x = int(ctx[s]), int(owned[s]), int(new[s])
+        c, x = int(ctx[s]), int(new[s])
+        b = max(int(owned[s]), -(-c // BS))
         if x < 0:
             for j in range(b):
                 ring[(head + count + gave) % nb] = tables[s, j]
@@ -46,7 +47,6 @@ def step(ctx, owned, new, ring, head, count, tables, total_rows, parents=None, w
             out["granted"].append(1)
             out["q_start"].append(min(rows, total_rows))
             continue
-        b = max(b, -(-c // BS))
         ok = c + x <= cap and rows + x <= total_rows and not (parents is not None and x > 64 * words)
         need = max(0, -(-(c + x) // BS) - b) if ok and x > 0 else 0
         want_so_far += need
@@ -59,7 +59,7 @@ def step(ctx, owned, new, ring, head, count, tables, total_rows, parents=None, w
         for i in range(min(x, max(total_rows - rows, 0))):
             t, r = c + i, rows + i
             out["positions"][r] = t
-            if ok:
+            if ok and tables[s, t // BS] >= 0:     # (an entry below 0 is no block)
                 out["slots"][r] = int(tables[s, t // BS]) * BS + t % BS
             if parents is not None and min(rows + x, total_rows) - rows <= 64 * words:
                 depth, at = 0, i

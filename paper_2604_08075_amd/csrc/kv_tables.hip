@@ -122,13 +122,12 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
     if (s + nt < B) x1 = a.fresh[s + nt], c1 = a.context[s + nt], b1 = a.owned[s + nt];
     const uint32_t n = (uint32_t)max(x, 0);
     c = (int)min((int64_t)max(c, 0), cap);
-    b = min(max(b, 0), a.max_blocks);
+    b = max(min(max(b, 0), a.max_blocks), (c + kBS - 1) / kBS);
     const uint32_t n_upto = wave_scan(n, a.rows + 1, wsum[0]);
     const uint32_t back_upto = wave_scan(x < 0 ? (uint32_t)b : 0, nb, wsum[1]);
     __syncthreads();
     const uint32_t rows_end = join_waves(n_upto, a.rows + 1, wsum[0], rows_c);
     const uint32_t back_end = join_waves(back_upto, nb, wsum[1], back_c);
-    b = max(b, (c + kBS - 1) / kBS);
     const int64_t want = (int64_t)c + n;
     const bool fits = want <= cap && rows_end <= a.rows && !(a.parents && n > 64u * a.words);
     const uint32_t need = fits && x > 0 ? (uint32_t)max((int64_t)0, (want + kBS - 1) / kBS - b) : 0;

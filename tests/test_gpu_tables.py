@@ -155,3 +155,24 @@ def test_tables_trees_of_a_large_batch(gpu_lib):
     want = tables.step(ctx, owned, new, ring, head, 500, tb, rows, par, 1)
     assert 0 < want["granted"].sum() < B
     same(run(gpu_lib, ctx, owned, new, ring, head, 500, tb, rows, par, 1), want)
+
+
+@pytest.mark.parametrize("B", [1, 6, 300, 700])
+def test_tables_owned_counts_below_the_context(gpu_lib, B):
+    """A count of blocks below what the cached tokens take stands for that, also where the sequence ends."""
+    note(f"tables, owned counts too small, B={B}")
+    rng = np.random.default_rng(B)
+    mb, free = 12, 200
+    ctx, owned, tb, ring, head = state(rng, B, mb, free)
+    ctx[0] = 16 * owned[0]
+    said = np.where(rng.random(B) < 0.7, rng.integers(-1, 3, B), owned)
+    said[0] = 0
+    new = np.where(rng.random(B) < 0.5, -1, rng.integers(0, 20, B))
+    new[0] = -1
+    rows = int(np.maximum(new, 0).sum()) + 1
+    want = tables.step(ctx, said, new, ring, head, free, tb, rows)
+    held = np.maximum(said, -(-ctx // 16))
+    over = new < 0
+    took = int((want["owned"] - held)[~over].sum())
+    assert want["state"][1] == free - took + int(held[over].sum()) and held[over].sum() > np.maximum(said, 0)[over].sum()
+    same(run(gpu_lib, ctx, said, new, ring, head, free, tb, rows, repeat=2), want)

@@ -173,3 +173,14 @@ def test_accept_by_scalar_moves():
                     ek[bt[s][dst // 16], g, dst % 16, d] = K[bt[s][src // 16], g, src % 16, d]
                     ev[bt[s][dst // 16], g, d, dst % 16] = V[bt[s][src // 16], g, d, src % 16]
     assert (k == ek).all() and (v == ev).all()
+
+
+# ---------------------------------------------------------------- counts that a context corrects
+
+def test_tables_owned_counts_below_the_context():
+    ring = np.array([70, 71, 72, 73, 0, 0, 0, 0])
+    tb = np.array([[10, 11, 12], [13, 14, -1], [15, -1, -1]])
+    o = tables.step([40, 20, 3], [1, 0, -1], [-1, 13, -1], ring, 0, 4, tb, 13)
+    assert o["ring"].tolist() == [70, 71, 72, 73, 10, 11, 12, 15] and o["state"].tolist() == [1, 7]
+    assert o["owned"].tolist() == [0, 3, 0] and o["tables"][1].tolist() == [13, 14, 70]
+    assert o["slots"][-1] == 70 * 16
