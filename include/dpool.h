@@ -520,7 +520,9 @@ int kv_tables_step(const int32_t* context_lens, const int32_t* n_owned, const in
 /*     k_blocks[blk, g, slot, :] = enc(y' / k_scale[g])                      */
 /*     v_blocks[blk, g, :, slot] = enc(v[r, g, :] / v_scale[g])              */
 /* with blk = slots[r] / 16, slot = slots[r] % 16; enc() rounds to bf16, or */
-/* as in kv_cache_append to e4m3.  All arithmetic is fp32, rounded once.    */
+/* as in kv_cache_append to e4m3.  Values need not be finite: a NaN, also    */
+/* one that the norm of an infinity makes, is stored as NaN, an infinity as  */
+/* +-448 in e4m3.  All arithmetic is fp32, rounded once.                     */
 /* A row whose position is outside [0, n_positions) is left alone            */
 /* altogether; one whose slot is outside [0, 16 * num_blocks) writes q_out   */
 /* and no cache.  Two rows that name the same slot race.                     */

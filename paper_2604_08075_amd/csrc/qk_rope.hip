@@ -66,9 +66,11 @@ __device__ __forceinline__ int pack_bf16(float a, float b) {
   return __builtin_bit_cast(int, p);
 }
 
-// Four values to e4m3 codes: clamped (the conversion does not saturate), to nearest even
+// Four values to e4m3 codes: clamped (the conversion does not saturate), to nearest even.
+// A NaN stays one, which fmin and fmax would make a number: the norm of a head with an
+// infinity is NaN, and a -448 in its place would pass for a key.
 __device__ __forceinline__ int pack_e4m3(float a, float b, float c, float d) {
-  const auto cut = [](float x) { return fminf(fmaxf(x, -kE4M3Max), kE4M3Max); };
+  const auto cut = [](float x) { return x != x ? x : fminf(fmaxf(x, -kE4M3Max), kE4M3Max); };
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(cut(a), cut(b), 0, false);
   return __builtin_amdgcn_cvt_pk_fp8_f32(cut(c), cut(d), r, true);
 }

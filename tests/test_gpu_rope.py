@@ -192,3 +192,40 @@ def test_infinities_stay_in_their_head(gpu_lib):
     assert diff.tolist() == [[3, 1, 100]]            # without a norm, dimension 100 is not turned
     assert (np.argwhere(ak != bk)[:, :3] == [85 // 16, 0, 85 % 16]).all()
     assert np.argwhere(av != bv).tolist() == [[34 // 16, 1, 7, 34 % 16]]
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("rows", [1, 37, 300, 4200])
+def test_nan_stays_nan_in_an_e4m3_cache(gpu_lib, rows, norm):
+    """A NaN, given or made by the norm of an infinity, is stored as a NaN code; an infinity as the largest value."""
+    note(f"rope, NaN into an e4m3 cache, rows={rows} norm={norm}")
+    rng = np.random.default_rng(rows)
+    hq, hkv, nb = 2, 3, rows // 16 + 3
+    q, k, v = codes(rng, rows, hq, 128), codes(rng, rows, hkv, 128), codes(rng, rows, hkv, 128)
+    hit = rng.choice(rows, min(rows, 40), replace=False)
+    for i, r in enumerate(hit):
+        k[r, i % hkv, int(rng.integers(0, 128))] = (0x7FC0, 0x7F80, 0xFF80)[i % 3]
+        v[r, i % hkv, int(rng.integers(0, 128))] = (0xFFC0, 0x7F80, 0xFF80)[i % 3]
+    w = codes(rng, 128) if norm else None
+    ks, vs = ((rng.random(hkv) * 0.05 + 0.01).astype(np.float32) for _ in range(2))
+    table = rope.table(rows, 64).astype(np.float32)
+    pos, slots = np.arange(rows, dtype=np.int32), np.arange(3, rows + 3, dtype=np.int64)
+    kp, vp = dev(np.zeros((nb, hkv, 16, 128), np.uint8)), dev(np.zeros((nb, hkv, 128, 16), np.uint8))
+    out = dev(np.zeros_like(q))
+    gpu_lib.qk_norm_rope_append(dev(q), dev(k), dev(v), dev(table), dev(pos), dev(slots), out, kp, vp,
+                                gpu_lib.qk_shape(rows, hq, hkv, nb, rows, 64, kv_fp8=True), None,
+                                dev(w) if norm else None, 1e-6, dev(ks), dev(vs))
+    torch.cuda.synchronize()
+    t = table.astype(np.float64)
+    with np.errstate(invalid="ignore"):
+        want_k = rope.turn(rope.norm(numerics.decode_bf16(k), numerics.decode_bf16(w) if norm else None, 1e-6),
+                           t[:, :32], t[:, 32:]) / ks.astype(np.float64)[:, None]
+        want_v = numerics.decode_bf16(v) / vs.astype(np.float64)[:, None]
+    assert np.isnan(want_k).any() and np.isnan(want_v).any()
+    s = slots
+    got_k = kp.cpu().numpy()[s // 16, :, s % 16]
+    got_v = vp.cpu().numpy()[s // 16, :, :, s % 16]
+    for got, want in ((got_k, want_k), (got_v, want_v)):
+        assert np.array_equal((got & 0x7F) == 0x7F, np.isnan(want))
+        big = np.isinf(want)
+        assert np.array_equal(got[big], np.where(want[big] < 0, 0xFE, 0x7E))
