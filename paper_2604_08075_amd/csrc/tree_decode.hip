@@ -679,10 +679,16 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs a) {
       if (p.c0 + col >= p.q.n * a.group) continue;
       if (whole) {
         const float l = st.lsum[b][0];
-        const float inv = l == 0.f ? 0.f : vsc / l;  // a row that sees no token: zeros
+        const bool none = l == 0.f;  // sees no token, or all its scores are -infinity: zeros, whatever V holds
+        const float inv = none ? 0.f : vsc / l;
+        if (none) {
+#pragma unroll
+          for (int nn = 0; nn < 8; ++nn) st.acc[b][nn] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 #pragma unroll
         for (int nn = 0; nn < 8; nn += 2)
-          store_out<FP8>(a, p.s, p.g, p.q, p.c0 + col, 16 * nn + 8 * lj, st.acc[b][nn] * inv, st.acc[b][nn + 1] * inv, odd_v);
+          store_out<FP8>(a, p.s, p.g, p.q, p.c0 + col, 16 * nn + 8 * lj, st.acc[b][nn] * inv, st.acc[b][nn + 1] * inv,
+                         odd_v && !none);
       } else {
         const size_t rec = (size_t)(2 * walk.wg + (p.j0 == 0)) * COLS + col;
         if (lj == 0) *(f32x4*)(a.stat + 4 * rec) = f32x4{st.mc[b], st.lsum[b][0], odd_v ? 1.f : 0.f, 0.f};
@@ -750,8 +756,10 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int cols) {
   add(s1);
 #pragma unroll 4
   for (int p = wg + 2; p <= d.last; ++p) add(read(2 * p));
-  const float inv = l == 0.f ? 0.f : vsc / l;
-  store_out<FP8>(a, d.s, d.g, q, cc, dim, o0 * inv, o1 * inv, odd);
+  const bool none = l == 0.f;
+  const float inv = none ? 0.f : vsc / l;
+  if (none) o0 = o1 = f32x4{0.f, 0.f, 0.f, 0.f};
+  store_out<FP8>(a, d.s, d.g, q, cc, dim, o0 * inv, o1 * inv, odd && !none);
 }
 
 }  // namespace dpool_tree

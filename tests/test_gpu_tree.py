@@ -295,3 +295,27 @@ def test_row_offsets_out_of_order(gpu_lib, B, fmt):
     n = np.diff(ordered)
     # (at most as many rows as a sequence has tokens)
     assert np.isfinite(want).any() and np.isnan(want).all((1, 2)).sum() == total - np.minimum(n, [t for _, t in chunks]).sum()
+
+
+@pytest.mark.parametrize("fmt", FMT)
+@pytest.mark.parametrize("T,n", [(40, 3), (70, 9), (5, 5), (2600, 4)])
+def test_scores_of_minus_infinity_give_zeros(gpu_lib, T, n, fmt):
+    """Rows whose scores are all -infinity are zero, whatever V holds; the other heads keep their bits."""
+    note(f"tree, scores of -infinity, T={T} n={n} {fmt}")
+    w = workloads.make_prefill([(n, T), (n, T)], 4, 2, c_max=T, kv_format=fmt, seed=71)
+    mask = tree_masks(np.random.default_rng(7), [n, n], 1, "tree")
+    K, V = w.k_store.dense().copy(), w.v_store.dense().copy()
+    one, nan = (0x3F80, 0x7FC0) if fmt == "bf16" else (0x38, 0x7F)
+    K[:, 0] = one                          # KV head 0: every key is 1, the first sequence's queries are -infinity
+    w.q_bits[:n, :2] = 0xFF80
+    conv = (lambda x: torch.from_numpy(x.view(np.int16))) if fmt == "bf16" else torch.from_numpy
+    d = workloads.to_device(w)
+    d["k"] = conv(K)[None].cuda()
+    clean = call(gpu_lib, w, d, mask, 1)
+    assert (clean[:n, :2] == 0).all() and np.isfinite(clean).all() and (clean[n:] != 0).any()
+    for t in (0, T - n, T - 1):            # committed and drafted
+        V[w.block_tables[0][t // 16], 0, 3:5, t % 16] = nan
+    if fmt == "bf16":
+        V[w.block_tables[0][(T - n) // 16], 0, 9, (T - n) % 16] = 0x7F80
+    d["v"] = conv(V)[None].cuda()
+    assert np.array_equal(call(gpu_lib, w, d, mask, 1), clean)
