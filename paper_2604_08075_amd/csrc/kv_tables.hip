@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
     if (s + nt < B) x1 = a.fresh[s + nt], c1 = a.context[s + nt], b1 = a.owned[s + nt];
     const uint32_t n = (uint32_t)max(x, 0);
     c = (int)min((int64_t)max(c, 0), cap);
-    b = max(min(max(b, 0), a.max_blocks), (c + kBS - 1) / kBS);
+    b = max(min(max(b, 0), a.max_blocks), (int)((uint32_t)(c + kBS - 1) / kBS));
     const uint32_t n_upto = wave_scan(n, a.rows + 1, wsum[0]);
     const uint32_t back_upto = wave_scan(x < 0 ? (uint32_t)b : 0, nb, wsum[1]);
     __syncthreads();
