@@ -634,12 +634,16 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs a) {
     // already): else the compiler would wait for all loads in every step.
     __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0)
     if constexpr (FP8) {
-      if (cmul < 0.f) {  // a scale below 0: the queries change sign instead (-inf hides a token, the largest score leads)
-        cmul = -cmul;
+      // A scale below 0: the queries change sign instead (-inf hides a token, the largest score leads).
+      // A NaN: the queries become NaN instead (the scale would make one of a hidden token's -inf).
+      if (!(cmul > 0.f)) {
+        const bool nan = cmul != cmul;
+        const int flip = nan ? 0 : (int)0x80008000, fill = nan ? 0x7fff7fff : 0;
+        cmul = nan ? 1.f : -cmul;
 #pragma unroll
         for (int b = 0; b < NC; ++b)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) st.qf[b][c] ^= (int)0x80008000;
+          for (int c = 0; c < 4; ++c) st.qf[b][c] = (st.qf[b][c] ^ flip) | fill;
       }
     }
     lds_barrier();

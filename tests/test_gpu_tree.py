@@ -319,3 +319,17 @@ def test_scores_of_minus_infinity_give_zeros(gpu_lib, T, n, fmt):
         V[w.block_tables[0][(T - n) // 16], 0, 9, (T - n) % 16] = 0x7F80
     d["v"] = conv(V)[None].cuda()
     assert np.array_equal(call(gpu_lib, w, d, mask, 1), clean)
+
+
+def test_key_scale_that_is_not_a_number(gpu_lib):
+    """A row that sees no token is zero under any scale; the other rows of that KV head are NaN."""
+    note("tree, e4m3 with a key scale of NaN")
+    chunks = [(3, 50), (4, 4), (9, 700)]
+    w = workloads.make_prefill(chunks, 4, 2, c_max=704, kv_format="fp8_e4m3", seed=53)
+    mask = tree_masks(np.random.default_rng(2), [3, 4, 9], 1, "tree")
+    mask[4] = 0
+    good = call(gpu_lib, w, workloads.to_device(w), mask, 1)
+    w.k_scale = w.k_scale * np.float32([np.nan, 1])
+    got = call(gpu_lib, w, workloads.to_device(w), mask, 1)
+    assert np.array_equal(got[:, 2:], good[:, 2:]) and (good[4] == 0).all()
+    assert (got[4, :2] == 0).all() and np.isnan(np.delete(got[:, :2], 4, axis=0)).all()
