@@ -198,3 +198,46 @@ def test_outputs_that_are_inputs_refused(host_lib):
         assert accept(host_lib, out=9 * P, **{name: 9 * P}) == EINVAL
     for name in ("k", "v"):
         assert qk(host_lib, {name: 2 * P}) == EINVAL and "q_out" in host_lib.last_error()
+
+
+def test_binding_refuses_rows_at_other_strides(host_lib):
+    """Slices of one projection with the strides of tensors of their own would read other rows' values."""
+    import torch
+    rows, hq, hkv = 5, 4, 2
+    qkv = torch.zeros(rows, (hq + 2 * hkv) * 128, dtype=torch.bfloat16)
+    sliced = qkv.split([hq * 128, hkv * 128, hkv * 128], dim=1)
+    own = [x.contiguous() for x in sliced]
+    x = torch.zeros(rows, dtype=torch.int64)
+
+    def call(tensors, out=None, n=rows, **strides):
+        # (a shape that the library refuses: what gets that far was not refused for its strides)
+        s = host_lib.qk_shape(n, hq, hkv, 64, 100, **strides)
+        s.reserved = 1
+        out = torch.zeros(rows, hq, 128, dtype=torch.bfloat16) if out is None else out
+        host_lib.qk_norm_rope_append(*tensors, torch.zeros(100, 128), x, x, out, x, x, s, stream=0)
+
+    wide = dict(q_stride=1024, k_stride=1024, v_stride=1024)
+    heads = lambda ts: [t.unflatten(1, (-1, 128)) for t in ts]  # noqa: E731
+    for tensors, strides in ((own, {}), (sliced, wide), (heads(own), {}), (heads(sliced), wide),
+                             ([t.reshape(-1, 128) for t in own], {}), ([t.flatten() for t in own], {}),
+                             ([qkv.flatten()] * 3, wide), ([t[:, None] for t in heads(sliced)], wide),
+                             ([t[None] for t in heads(sliced)], wide),
+                             ([t.unflatten(0, (1, rows)) for t in sliced], wide)):
+        with pytest.raises(host_lib.DpoolError):
+            call(tensors, **strides)
+    two = torch.zeros(2, 3, (hq + 2 * hkv) * 128)               # rows of two dimensions
+    with pytest.raises(host_lib.DpoolError):
+        call(two.split([hq * 128, hkv * 128, hkv * 128], dim=2), n=6, **wide)
+    with pytest.raises(host_lib.DpoolError):
+        call([t[:1] for t in sliced], n=1)                      # one row: no stride to speak of
+    for i in range(3):
+        for bad in (sliced[i], heads(sliced)[i], own[i][::2], own[i].unflatten(1, (-1, 128)).flip(0).transpose(1, 2),
+                    heads(own)[i].transpose(0, 1), own[i][:1].expand(rows, -1)):
+            with pytest.raises(ValueError, match="strides"):
+                call([bad if j == i else own[j] for j in range(3)])
+        with pytest.raises(ValueError, match="strides"):
+            call([own[i] if j == i else sliced[j] for j in range(3)], **wide)
+        with pytest.raises(ValueError, match="strides"):        # every other row
+            call([two[:, ::2].split([hq * 128, hkv * 128, hkv * 128], dim=2)[j] for j in range(3)], n=4, **wide)
+    with pytest.raises(ValueError, match="contiguous"):
+        call(own, out=torch.zeros(rows, hq, 256, dtype=torch.bfloat16)[..., :128])
