@@ -10,7 +10,7 @@
 // and lane + 64, and a moved value passes from one word of its registers to
 // another.  Measured: paths of up to eight of sixteen drafts, 128 sequences, 16
 // layers, 8 heads, bf16 (56 MB of values; counted 108 MB read, 81 MB written):
-// 45 us, 4.2 TB/s (a large copy: 4.8); value by value it was 60.  Paths of up to
+// 43 us, 4.4 TB/s (a large copy: 4.8); value by value it was 60.  Paths of up to
 // five, five sequences, 6 layers, 4 heads, e4m3: 4.7 us.
 //
 // Entries are strictly increasing, accepted[j] >= j, and only one wave works

@@ -12,9 +12,9 @@
 // workgroup scans the whole batch by itself (the lengths come from L2, a batch
 // of 256 in one go), and then takes its share of the rows: no workgroup waits
 // for another, and there is no second launch.  Measured, per call: 256 single
-// tokens 5.8 us, 96 trees of up to 32 drafts 7.2, 512 prompts of 722,154 tokens
-// (9 MB of slots, positions and tables, 0.9 TB/s) 10.4; with ten barriers a scan
-// and wave sums by permutes instead of two and lane shifts 7.0, 7.7 and 12.0.
+// tokens 6.0 us, 96 trees of up to 32 drafts 6.4, 512 prompts of 722,154 tokens
+// (9 MB of slots, positions and tables, 1.0 TB/s) 9.1; with ten barriers a scan
+// and wave sums by permutes instead of two and lane shifts 1.2, 0.5 and 1.6 more.
 // A row's sequence is found by a binary search over the running sums in LDS.
 //
 // Nothing that the call reads is written by it (the ring's tail and the table

@@ -405,6 +405,8 @@ extern "C" int qk_norm_rope_append(const void* q, const void* k, const void* v, 
   // 256 single tokens 8.5 / 9.0 / 16.2; 256 trees of four 17.8 / 13.9 / 14.8;
   // 4,096 tokens of four prompts 84 / 51 / 43, as 4,096 single tokens 106 / 100 /
   // 114; 8,192 tokens of prompts 160 / 94 / 78 (5.4 TB/s; a large copy reaches 4.8).
+  // The host sees rows and not their slots: thousands of single tokens pay for what
+  // prompts gain.  Other head counts were not measured beside the rule.
   const bool paired = sh->interleaved == 1;
   hipStream_t st = (hipStream_t)stream;
   if (sh->rows <= 256) launch<1, 1>(a, fp8, paired, st);

@@ -18,7 +18,12 @@
 //     2^kSlack, so the common path has no rescale.
 //   * probabilities are rounded to bf16, the operand's type; the denominator is
 //     a product against ones that sums the rounded ones, so that every output
-//     is a convex combination of V rows.  All sums are fp32.
+//     is a convex combination of V rows.  All sums are fp32.  That rounding
+//     makes the error against 64 bits 2.3e-3 of the norm where rounding the
+//     result alone makes 1.7e-3.  A second product with what it takes away gave
+//     1.7e-3 and cost 1.5% of the time with 64 columns (181 us -> 183.5), 31%
+//     with 256 (424 -> 556) and 33% in e4m3 with 128 (141 -> 188), so it is not
+//     made; fp16 holds neither all of V nor the small probabilities of long contexts.
 // All tiles of all items are cut into one slice of equal cost per workgroup; an
 // item that a cut goes through leaves sums (maximum, denominator, o) that a
 // second kernel joins, in order, so results do not depend on timing.
@@ -26,13 +31,16 @@
 // What bounds it, measured on one MI355X (a large read reaches 6.6 TB/s, a
 // large bf16 product 1,212 TFLOP/s): 64 columns (eight drafts, GQA 8) memory:
 // sixteen contexts of 32,768 tokens, bf16, 411 us, 5.2 TB/s.  The short pool's
-// 128 ragged contexts 186 us: 1.4 us a tile and workgroup, 6 us for every end
+// 128 ragged contexts 181 us: 1.4 us a tile and workgroup, 6 us for every end
 // of an item, 8 us before the first tile and 13 for the join and its launch.
-// 256 columns: neither alone; the matrix cores are busy half the time (32 drafts
-// on sixteen contexts of 65,536 tokens: 1,294 us, 850 TFLOP/s; e4m3, sixteen
-// drafts, GQA 16: 977).  Four tiles on their way instead of two, and scores,
-// probabilities and products of three tiles interleaved by hand, came to the
-// same within 4%, so the plain order stays.
+// 256 columns: neither alone; the matrix cores are busy a third of the time (32
+// drafts on sixteen contexts of 65,536 tokens: 1,294 us, 850 TFLOP/s; e4m3,
+// sixteen drafts, GQA 16: 977).  Scores, softmax and output products of a tile
+// follow each other, and each of K's operands is waited for as it is read from
+// LDS (V's eight are read together).  Variants with four tiles on their way, and
+// with three tiles' steps interleaved by hand, were within 4% and not kept; they
+// read K the same way, so they show no bound.  The 128-column variants spill four
+// (bf16) and six (e4m3) registers, stored and loaded at the ends of a piece.
 //
 // LDS: K's sixteen 16-byte chunks of a token are stored exclusive-or'ed with
 // (token % 4, token / 8 % 4), V's with bit 4 of the dimension, so that the
@@ -840,7 +848,11 @@ Plan plan(const dp_tree_shape* sh) {
   // / 192 / 198; 16 to 208 (short pool, e4m3, 112 on average) 170 / 155 / 173; 256
   // (long pool, bf16) 900 / 530 / 440.  Two workgroups of four waves to a compute
   // unit fill each other's gaps (one: 207 for 186, 213 for 162); eight waves of 32
-  // columns leave registers for one.
+  // columns leave registers for one.  Trees of one size, short pool, bf16, 64 / 72 /
+  // 128 / 136 / 256 columns: 181 / 194 / 219 / 241 / 285; e4m3, 64 / 80 / 128 / 144 /
+  // 256: 92 / 107 / 128 / 162 / 192.  Trees above the width that the average gives
+  // take several items, each of which reads the cache again: one tree of 512 columns
+  // on the longest of 128 contexts, the others of 32: 174 for 167.
   if (per_seq <= 64) return Plan{0, 64, 2 * cus};
   if (per_seq <= 128) return Plan{1, 128, 2 * cus};
   return Plan{2, 256, cus};
