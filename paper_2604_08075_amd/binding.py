@@ -429,10 +429,14 @@ def qk_shape(rows, n_q_heads, n_kv_heads, num_blocks, n_positions, rotary_dim=12
                    n_kv_heads * head_dim if v_stride is None else v_stride)
 
 
-def _check_rows(name, t, heads, head_dim, stride) -> None:
-    """Refuses a tensor whose rows of heads * head_dim values do not lie `stride` elements apart."""
+def _check_rows(name, t, n, heads, head_dim, stride) -> None:
+    """Refuses a tensor whose n rows of heads * head_dim values do not lie `stride` elements apart."""
+    if t.numel() == 0:
+        return
     width, inner, rows = heads * head_dim, 1, 1
     for size, step in zip(reversed(t.shape), reversed(t.stride())):
+        if inner >= width and rows >= n:  # (further rows are not read, whatever lies between them)
+            return
         if size != 1 and step != (inner if inner < width else stride * rows):
             raise ValueError(f"{name} has strides {tuple(t.stride())}, the shape's rows of {width} lie {stride} apart")
         if inner < width:
@@ -450,9 +454,9 @@ def qk_norm_rope_append(q, k, v, cos_sin, positions, slots, q_out, k_blocks, v_b
     qs, ks, vs = shape.q_stride, shape.k_stride, shape.v_stride
     # ([rows, heads, 128] is compared first, all three at once: 0.5 us of the host)
     if (q.stride(), k.stride(), v.stride()) != ((qs, 128, 1), (ks, 128, 1), (vs, 128, 1)):
-        _check_rows("q", q, shape.n_q_heads, shape.head_dim, qs)
-        _check_rows("k", k, shape.n_kv_heads, shape.head_dim, ks)
-        _check_rows("v", v, shape.n_kv_heads, shape.head_dim, vs)
+        _check_rows("q", q, shape.rows, shape.n_q_heads, shape.head_dim, qs)
+        _check_rows("k", k, shape.rows, shape.n_kv_heads, shape.head_dim, ks)
+        _check_rows("v", v, shape.rows, shape.n_kv_heads, shape.head_dim, vs)
     if not q_out.is_contiguous():
         raise ValueError("q_out must be contiguous")
     check(lib().qk_norm_rope_append(

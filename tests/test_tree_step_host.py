@@ -241,3 +241,21 @@ def test_binding_refuses_rows_at_other_strides(host_lib):
             call([two[:, ::2].split([hq * 128, hkv * 128, hkv * 128], dim=2)[j] for j in range(3)], n=4, **wide)
     with pytest.raises(ValueError, match="contiguous"):
         call(own, out=torch.zeros(rows, hq, 256, dtype=torch.bfloat16)[..., :128])
+
+
+def test_binding_takes_rows_that_no_stride_reaches(host_lib):
+    """No rows, or the first of many: what lies between rows does not matter then."""
+    import torch
+    x = torch.zeros(5, dtype=torch.int64)
+    qkv = torch.zeros(5, 8 * 128, dtype=torch.bfloat16)
+    for rows, given in ((0, qkv[:0]), (0, torch.zeros(0)), (1, qkv), (1, qkv.unflatten(1, (-1, 128)))):
+        q, k, v = (given[:, :4], given[:, 4:6], given[:, 6:]) if given.dim() == 3 else (
+            (given[:, :512], given[:, 512:768], given[:, 768:]) if given.dim() == 2 else (given,) * 3)
+        s = host_lib.qk_shape(rows, 4, 2, 64, 100)
+        s.reserved = 1          # refused by the library: got as far as that
+        with pytest.raises(host_lib.DpoolError):
+            host_lib.qk_norm_rope_append(q, k, v, x, x, x, torch.zeros(5, 4, 128), x, x, s, stream=0)
+    s = host_lib.qk_shape(2, 4, 2, 64, 100)
+    with pytest.raises(ValueError, match="strides"):
+        host_lib.qk_norm_rope_append(qkv[:, :512], qkv[:, 512:768], qkv[:, 768:], x, x, x, torch.zeros(5, 4, 128), x, x,
+                                     s, stream=0)
