@@ -495,6 +495,8 @@ class CacheLayers:
     def __init__(self, k_layers, v_layers):
         if len(k_layers) != len(v_layers):
             raise ValueError("as many K as V caches")
+        if not all(t.is_contiguous() for t in (*k_layers, *v_layers)):
+            raise ValueError("caches must be contiguous")
         self.tensors = (list(k_layers), list(v_layers))
         self.n = len(k_layers)
         self.k, self.v = ((ctypes.c_void_p * self.n)(*[t.data_ptr() for t in ts]) for ts in self.tensors)

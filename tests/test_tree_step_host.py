@@ -259,3 +259,15 @@ def test_binding_takes_rows_that_no_stride_reaches(host_lib):
     with pytest.raises(ValueError, match="strides"):
         host_lib.qk_norm_rope_append(qkv[:, :512], qkv[:, 512:768], qkv[:, 768:], x, x, x, torch.zeros(5, 4, 128), x, x,
                                      s, stream=0)
+
+
+def test_binding_refuses_caches_with_gaps(host_lib):
+    """Layers interleaved in one tensor are no caches of their own: tokens would move in other layers' blocks."""
+    import torch
+    both = torch.zeros(4, 2, 2, 16, 128)
+    k, v = [both[:, i] for i in range(2)], [x.contiguous() for x in both.transpose(3, 4).unbind(1)]
+    for a, b in ((k, v), (v, k)):
+        with pytest.raises(ValueError, match="contiguous"):
+            host_lib.CacheLayers(a, b)
+    apart = both.transpose(0, 1).contiguous()
+    assert host_lib.CacheLayers(list(apart), v).n == 2
