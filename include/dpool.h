@@ -640,7 +640,8 @@ int tree_decode_attention(const void* q, const void* k_blocks, const void* v_blo
 /* leaves the sequence alone, context_lens_out[s] = T (for one that          */
 /* kv_tables_step refused: it has rows, but no cached drafts).  Codes are    */
 /* moved as they are.  A token whose block id is outside the pool is not     */
-/* moved.                                                                    */
+/* moved.  Offsets of q_start out of order, a broken promise, are clamped    */
+/* pair by pair here: n may differ from the attention's then.                */
 /*   k_layers, v_layers  host arrays of n_layers device pointers, caches as */
 /*                       for kv_cache_append, all of one shape, no two the  */
 /*                       same (DP_EINVAL); read during the call only         */
