@@ -257,6 +257,7 @@ int dp_cost_model(double lambda, double alpha, double mu_short, double mu_long, 
 /* ------------------------------------------------------------------------ */
 #define DP_KV_BF16 0
 #define DP_KV_FP8_E4M3 1
+#define DP_KV_FP8_E4M3_BLOCK 2 /* e4m3, a scale per block and head: only the entry points that name it */
 #define DP_OUT_BF16 0
 #define DP_OUT_FP32 1
 
@@ -339,6 +340,48 @@ int paged_decode_attention_noalloc(const void* q, const void* k_blocks, const vo
                                    const int32_t* block_tables, const int32_t* context_lens,
                                    float scale, const float* k_scale, const float* v_scale,
                                    void* out, const dp_decode_shape* shape, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Decode over a sliding window, and over block scales (device, asynchronous)*/
+/*                                                                           */
+/* Layers of long-context models that see a window read, for every           */
+/* generated token, the window's part of the cache instead of all of it, and */
+/* a few first tokens that stay visible.  For sequence s with                */
+/* T = context_lens[s]:                                                       */
+/*   out[s,h,:] = sum_t softmax_t(scale * q[s,h,:] . K_t) V_t                */
+/*   over T - window <= t < T, and t < min(n_sink, T)                        */
+/* T = 0 gives a zero row, and so does one whose scores are all -infinity.   */
+/* A cached value of a token that is not seen never reaches the result,      */
+/* finite or not, and table entries of blocks that hold no token that is     */
+/* seen are never read (blocks that have left the window may go back to the  */
+/* pool).  window >= 1; one of max_context_len or more hides nothing.        */
+/* n_sink >= 0.                                                               */
+/*                                                                           */
+/* kv_dtype may also be DP_KV_FP8_E4M3_BLOCK: the cache holds e4m3 codes as  */
+/* for DP_KV_FP8_E4M3, and k_scale, v_scale are [num_blocks, n_kv_heads]     */
+/* bytes, the exponents of powers of two (OCP E8M0):                          */
+/*   K_t = 2^(k_scale[blk][g] - 127) * k_blocks[blk, g, t%16, :]             */
+/*   V_t = 2^(v_scale[blk][g] - 127) * v_blocks[blk, g, :, t%16]             */
+/* with blk = block_tables[s][t/16]; 255 stands for NaN.  Such a cache needs */
+/* no calibration: qk_norm_rope_append_scaled sets the scales.  Values are   */
+/* taken as bf16, which holds them exactly but for those below 2^-126 (a few */
+/* bits fewer) and above its largest (infinity).                              */
+/*                                                                           */
+/* Everything else, the shape, layouts, split, workspace and its rules,      */
+/* limits and errors, is as for paged_decode_attention, and the two may      */
+/* share a workspace; for DP_KV_FP8_E4M3 k_scale and v_scale are fp32        */
+/* [n_kv_heads] and 4-byte aligned.  Calls whose windows and sinks hold few  */
+/* tokens count as short whatever max_context_len is.  q, out and workspace  */
+/* do not overlap (DP_EINVAL where they start together).  DP_EINVAL for      */
+/* window < 1 or n_sink < 0.                                                  */
+/* ------------------------------------------------------------------------ */
+size_t window_decode_workspace_size(const dp_decode_shape* shape, int32_t window, int32_t n_sink);
+
+int window_decode_attention(const void* q, const void* k_blocks, const void* v_blocks,
+                            const int32_t* block_tables, const int32_t* context_lens, float scale,
+                            int32_t window, int32_t n_sink, const void* k_scale, const void* v_scale,
+                            void* out, const dp_decode_shape* shape, void* workspace,
+                            size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* KV-cache append (device, asynchronous).                                   */

@@ -20,6 +20,8 @@ precision:
   (Sec. 1.2: each pool runs chunked prefill internally).
 * ``append``    - the KV-cache append of each decode step, with OCP E4M3
   encoding for an FP8 cache (Sec. 4.4, Sec. 4.7).
+* ``window``    - attention over a sliding window with visible first tokens,
+  and the cache with a scale for each block.
 * ``pool``      - per-sequence KV bytes and concurrent-sequence count
   (Sec. 1.1, Eq. 1 and Eq. 2).
 * ``route``     - token-budget estimation, EMA calibration and pool dispatch

@@ -23,7 +23,7 @@ DP_EIO = -5
 DP_ENOMEM = -12
 DP_EINVAL = -22
 DP_ENOTSUP = -95
-KV_BF16, KV_FP8_E4M3 = 0, 1
+KV_BF16, KV_FP8_E4M3, KV_FP8_E4M3_BLOCK = 0, 1, 2
 OUT_BF16, OUT_FP32 = 0, 1
 
 # every function the header declares
@@ -33,7 +33,7 @@ EXPORTS = (
     "route_default_params", "route_init", "route_requests", "route_on_response",
     "route_adapt_default_params", "route_adapt_threshold", "dp_cost_model",
     "paged_decode_workspace_size", "paged_decode_partition_tokens", "paged_decode_attention",
-    "paged_decode_attention_noalloc",
+    "paged_decode_attention_noalloc", "window_decode_workspace_size", "window_decode_attention",
     "kv_cache_append", "chunked_prefill_attention", "kv_tables_step", "qk_norm_rope_append",
     "tree_decode_workspace_size", "tree_decode_attention", "kv_cache_accept", "dp_hbm_read_probe",
 )
@@ -158,6 +158,10 @@ def lib() -> ctypes.CDLL:
             ctypes.POINTER(DecodeShape), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         L.paged_decode_attention_noalloc.argtypes = [ctypes.c_void_p] * 5 + [ctypes.c_float] + [
             ctypes.c_void_p] * 3 + [ctypes.POINTER(DecodeShape), ctypes.c_void_p]
+        L.window_decode_workspace_size.argtypes = [ctypes.POINTER(DecodeShape), ctypes.c_int32, ctypes.c_int32]
+        L.window_decode_workspace_size.restype = ctypes.c_size_t
+        L.window_decode_attention.argtypes = [ctypes.c_void_p] * 5 + [ctypes.c_float] + [ctypes.c_int32] * 2 + [
+            ctypes.c_void_p] * 3 + [ctypes.POINTER(DecodeShape), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         L.kv_cache_append.argtypes = [ctypes.c_void_p] * 8 + [ctypes.POINTER(DecodeShape), ctypes.c_void_p]
         L.chunked_prefill_attention.argtypes = [ctypes.c_void_p] * 6 + [ctypes.c_float] + [ctypes.c_void_p] * 3 + [
             ctypes.POINTER(PrefillShape), ctypes.c_void_p]
@@ -311,11 +315,16 @@ def cost_model(lam: float, alpha: float, mu_short: float, mu_long: float) -> Cos
 
 # ---------------------------------------------------------------- decode
 
+def _kv_dtype(kv_fp8, block_scales):
+    return KV_FP8_E4M3_BLOCK if block_scales else KV_FP8_E4M3 if kv_fp8 else KV_BF16
+
+
 def decode_shape(batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks, kv_fp8=False,
-                 out_fp32=False, partition_tokens=0, workgroups_per_cu=0, head_dim=128,
-                 block_size=16) -> DecodeShape:
+                 out_fp32=False, partition_tokens=0, workgroups_per_cu=0, head_dim=128, block_size=16,
+                 block_scales=False) -> DecodeShape:
+    """block_scales: an e4m3 cache with a scale for each block and head (window_decode_attention)."""
     return DecodeShape(batch, n_q_heads, n_kv_heads, head_dim, block_size, max_blocks_per_seq, max_context_len,
-                       KV_FP8_E4M3 if kv_fp8 else KV_BF16, OUT_FP32 if out_fp32 else OUT_BF16, partition_tokens,
+                       _kv_dtype(kv_fp8, block_scales), OUT_FP32 if out_fp32 else OUT_BF16, partition_tokens,
                        workgroups_per_cu, 0, num_blocks)
 
 
@@ -372,6 +381,22 @@ def paged_decode_attention_noalloc(q, k_blocks, v_blocks, block_tables, context_
         q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
         float(scale), k_scale.data_ptr() if k_scale is not None else None,
         v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape),
+        _stream_ptr(stream)))
+
+
+def window_workspace_size(shape: DecodeShape, window, n_sink=0) -> int:
+    return int(lib().window_decode_workspace_size(ctypes.byref(shape), window, n_sink))
+
+
+def window_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, scale, window, n_sink, out,
+                            shape: DecodeShape, workspace=None, k_scale=None, v_scale=None, stream=None) -> None:
+    """Enqueue the decode over a sliding window and the first n_sink tokens, or over block scales
+    (include/dpool.h, window_decode_attention)."""
+    ws_ptr, ws_bytes = _ws(workspace)
+    check(lib().window_decode_attention(
+        q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
+        float(scale), window, n_sink, k_scale.data_ptr() if k_scale is not None else None,
+        v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape), ws_ptr, ws_bytes,
         _stream_ptr(stream)))
 
 
@@ -550,6 +575,41 @@ class PagedDecoder:
                  stream=None):
         paged_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, scale, out, self.shape,
                                self.workspace, k_scale, v_scale, stream)
+        return out
+
+
+class WindowDecoder:
+    """Holds one decode shape with its window and its workspace; calling it enqueues the decode.
+
+    window, n_sink: the query sees the `window` tokens up to its own, and the
+    first n_sink; None: the whole context.  block_scales: the e4m3 cache has a
+    scale for each block and head.  Device memory for the workspace comes from
+    torch's allocator once, at construction, zero-filled as the library requires.
+    """
+
+    def __init__(self, batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks, window=None,
+                 n_sink=0, kv_fp8=False, block_scales=False, out_fp32=False, partition_tokens=0, workgroups_per_cu=0,
+                 device="cuda"):
+        import torch
+        self.shape = decode_shape(batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks,
+                                  kv_fp8, out_fp32, partition_tokens, workgroups_per_cu, block_scales=block_scales)
+        self.window = max(max_context_len, 1) if window is None else window
+        self.n_sink = n_sink
+        ws = window_workspace_size(self.shape, self.window, n_sink)
+        if ws == 0:
+            raise DpoolError(DP_EINVAL, last_error())
+        self.workspace = torch.zeros(ws, dtype=torch.uint8, device=device)
+        self.out_dtype = torch.float32 if out_fp32 else torch.bfloat16
+
+    def new_out(self, device="cuda"):
+        import torch
+        s = self.shape
+        return torch.empty((s.batch, s.n_q_heads, s.head_dim), dtype=self.out_dtype, device=device)
+
+    def __call__(self, q, k_blocks, v_blocks, block_tables, context_lens, scale, out, k_scale=None, v_scale=None,
+                 stream=None):
+        window_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, scale, self.window, self.n_sink,
+                                out, self.shape, self.workspace, k_scale, v_scale, stream)
         return out
 
 

@@ -57,6 +57,20 @@
 // Blocks past a sequence's last token are never loaded; tail slots of its
 // last block are masked by select (scores to -inf, values to 0), so poisoned
 // or stale cache contents cannot leak into the result.
+//
+// Windows (WIN): the query sees the `window` tokens up to its own and the
+// first n_sink tokens.  A segment's stream is then the units that hold such a
+// token, the sinks' before the window's (live_span): the walk, the slices and
+// the merge are those of a shorter sequence, and only the unit's place in the
+// context (real_unit), the blocks it may read (live_block) and the masks of
+// the two units at the window's and the sinks' edges know of the gap.
+//
+// Block scales (BLK): each (block, KV head) tile has an exponent byte e, its
+// values are code * 2^(e - 127).  The conversion to bf16 takes that factor as
+// an operand (v_cvt_scalef32_pk_bf16_fp8 uses the exponent field of a float),
+// so a scale costs the load of one byte per lane, unit and operand, and
+// nothing in the loop; the product is exact in bf16, as a code has four
+// significant bits.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -107,6 +121,9 @@ struct DecodeArgs {
   int32_t num_blocks_m1;        // num_blocks - 1 (block ids are clamped into range)
   int32_t out_fp32;
   int32_t min_chunk;            // minimum units per slice
+  const uint8_t* k_exp;         // [num_blocks, Hkv] exponent bytes (BLK)
+  const uint8_t* v_exp;
+  int32_t window, n_sink;       // tokens seen up to the query's own; first tokens seen (WIN; both at most max_ctx)
 };
 
 // Unit geometry: a unit is 16 KiB of K and V of one KV head.
@@ -122,6 +139,7 @@ struct Geo {
 struct UnitRegs {
   i32x4 k[8];
   i32x4 v[8];
+  int ke, ve;  // exponent bytes of this lane's K and V block (BLK)
 };
 
 __device__ __forceinline__ float xor_max(float x) {
@@ -133,12 +151,13 @@ __device__ __forceinline__ float xor_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// Eight e4m3 bytes -> eight bf16 (exact; every e4m3 value is a bf16 value).
-__device__ __forceinline__ bf16x8 fp8x8_to_bf16(int lo, int hi) {
-  bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-  bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-  bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+// Eight e4m3 bytes times a power of two -> eight bf16 (exact in bf16's normal
+// range: a code has four significant bits).
+__device__ __forceinline__ bf16x8 fp8x8_to_bf16(int lo, int hi, float pow2 = 1.0f) {
+  bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, pow2, false);
+  bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, pow2, true);
+  bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, pow2, false);
+  bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, pow2, true);
   bf16x8 r;
   r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1];
   r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
@@ -156,13 +175,59 @@ __device__ __forceinline__ unsigned live_mask(int w, int nv) {
   return k == kPerWord ? 0xffffffffu : (1u << (8 * kTokBytes * k)) - 1u;
 }
 
+// The same from one bit a token.
+template <int kTokBytes>
+__device__ __forceinline__ unsigned live_bytes(int w, unsigned live) {
+  constexpr int kPerWord = 4 / kTokBytes;
+  unsigned m = 0;
+  for (int x = 0; x < kPerWord; ++x)
+    if ((live >> (kPerWord * w + x)) & 1) m |= (kTokBytes == 1 ? 0xffu : 0xffffu) << (8 * kTokBytes * x);
+  return m;
+}
+
 __device__ __forceinline__ uint16_t f32_to_bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
 __device__ __forceinline__ int clamp_ctx(int c, int max_ctx) { return c < 0 ? 0 : (c > max_ctx ? max_ctx : c); }
 
-template <bool FP8>
-__device__ __forceinline__ int units_of(int ctx) {
-  return (ctx + Geo<FP8>::UT - 1) / Geo<FP8>::UT;
+// The units of a sequence of ctx tokens that the query sees.  Without a window
+// they are all of its units; with one, the first `head` (the sinks') and those
+// from unit head + gap on (the window's).
+struct Span {
+  int lo;    // first token of the window
+  int head;  // units before the gap
+  int gap;   // units that hold no token that is seen
+  int nus;   // units that do
+};
+template <bool FP8, bool WIN>
+__device__ __forceinline__ Span live_span(const DecodeArgs& a, int ctx) {
+  constexpr int UT = Geo<FP8>::UT;
+  Span sp{0, 0, 0, (ctx + UT - 1) / UT};
+  if constexpr (WIN) {
+    sp.lo = max(ctx - a.window, 0);
+    const int first = sp.lo / UT;
+    sp.head = min((a.n_sink + UT - 1) / UT, first);
+    sp.gap = first - sp.head;
+    sp.nus -= sp.gap;
+  }
+  return sp;
+}
+template <bool WIN>
+__device__ __forceinline__ int real_unit(const Span& sp, int j) {
+  return WIN && j >= sp.head ? j + sp.gap : j;
+}
+// The block of the sequence (an entry of its table) that stands for block b of
+// unit j (its place in the context).  A block with no token that is seen, past
+// the end or between the sinks and the window, is never fetched and its entry
+// never read: its lanes re-read a live block of the unit (same addresses as
+// other lanes of the same load instruction, so no extra memory traffic) and
+// its tokens are masked.
+template <bool FP8, bool WIN>
+__device__ __forceinline__ int live_block(const DecodeArgs& a, const Span& sp, int j, int b, int nb) {
+  const int first = j * Geo<FP8>::UB, blk = first + b;
+  if constexpr (!WIN) return blk < nb ? blk : first;
+  const int wb = sp.lo / kBlock;  // the window's first block
+  auto seen = [&](int x) { return x >= wb || x * kBlock < a.n_sink; };
+  return blk < nb && seen(blk) ? blk : (seen(first) ? first : wb);
 }
 
 // Partial records cross compute units on different XCDs, whose L2 caches are
@@ -460,13 +525,23 @@ __device__ __forceinline__ void lane_offsets(int li, int lj, int (&kofs)[8], int
   }
 }
 
+// The running maximum before the first score.  With a window a row may meet
+// nothing but scores of -infinity in a unit (an infinite key): a finite start
+// keeps -inf - -inf out of the exponents.
+template <bool WIN>
+constexpr float kNoScore = WIN ? -3.0e38f : -INFINITY;
+
 // One unit of a piece: scores of the unit's tokens from unit_tok0 on (those at
-// or past ctx_s masked), online softmax, output products.
-template <bool FP8>
-__device__ __forceinline__ void attend_unit(const UnitRegs& R, const i32x4 (&qv)[4], int unit_tok0, int ctx_s, int lj,
-                                            float cscale, float& m_run, float& l_part, f32x4 (&acc)[8]) {
+// or past ctx_s masked, and those from n_sink up to lo), online softmax, output
+// products.
+template <bool FP8, bool WIN, bool BLK>
+__device__ __forceinline__ void attend_unit(const UnitRegs& R, const i32x4 (&qv)[4], int unit_tok0, int ctx_s, int lo,
+                                            int n_sink, int lj, float cscale, float& m_run, float& l_part,
+                                            f32x4 (&acc)[8]) {
   constexpr int UT = Geo<FP8>::UT, NZ = Geo<FP8>::NZ;
-  const bool ragged = unit_tok0 + UT > ctx_s;
+  const bool ragged = unit_tok0 + UT > ctx_s || (WIN && unit_tok0 < lo && unit_tok0 + UT > n_sink);
+  const float kp2 = BLK ? __uint_as_float((unsigned)R.ke << 23) : 1.0f;
+  const float vp2 = BLK ? __uint_as_float((unsigned)R.ve << 23) : 1.0f;
   const int lane_tok0 = unit_tok0 + (FP8 ? 16 : 8) * lj;  // first unit token of this lane's scores
 
   // S^T = K Q^T: lane (li, lj) holds scores of head li for its NZ tokens
@@ -478,9 +553,9 @@ __device__ __forceinline__ void attend_unit(const UnitRegs& R, const i32x4 (&qv)
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj) {
         const i32x4 raw = R.k[2 * m + jj];
-        sacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw[0], raw[1]),
+        sacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw[0], raw[1], kp2),
                                                        __builtin_bit_cast(bf16x8, qv[2 * jj]), sacc, 0, 0, 0);
-        sacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw[2], raw[3]),
+        sacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw[2], raw[3], kp2),
                                                        __builtin_bit_cast(bf16x8, qv[2 * jj + 1]), sacc, 0, 0,
                                                        0);
       }
@@ -501,10 +576,16 @@ __device__ __forceinline__ void attend_unit(const UnitRegs& R, const i32x4 (&qv)
   }
   // live tokens among this lane's NZ tokens (all of them unless the unit is ragged)
   const int nv = ragged ? min(max(ctx_s - lane_tok0, 0), NZ) : NZ;
-  if (ragged)
+  unsigned live = (1u << NZ) - 1;  // (WIN) one bit a token
+  if (ragged) {
+    if constexpr (WIN) {
+      auto first = [&](int n) { return (1u << min(max(n - lane_tok0, 0), NZ)) - 1; };  // the tokens before token n
+      live = first(ctx_s) & (~first(lo) | first(n_sink));
+    }
 #pragma unroll
     for (int e = 0; e < NZ; ++e)
-      if (e >= nv) z[e] = -INFINITY;
+      if (WIN ? !((live >> e) & 1) : e >= nv) z[e] = -INFINITY;
+  }
 
   // online softmax (base 2) for head li over this unit's tokens
   float bmax = z[0];
@@ -533,7 +614,7 @@ __device__ __forceinline__ void attend_unit(const UnitRegs& R, const i32x4 (&qv)
   unsigned vmask[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
   if (ragged)
 #pragma unroll
-    for (int wd = 0; wd < 4; ++wd) vmask[wd] = live_mask<FP8 ? 1 : 2>(wd, nv);
+    for (int wd = 0; wd < 4; ++wd) vmask[wd] = WIN ? live_bytes<FP8 ? 1 : 2>(wd, live) : live_mask<FP8 ? 1 : 2>(wd, nv);
 #pragma unroll
   for (int nn = 0; nn < 8; ++nn) {
     i32x4 raw = R.v[nn];
@@ -541,15 +622,15 @@ __device__ __forceinline__ void attend_unit(const UnitRegs& R, const i32x4 (&qv)
 #pragma unroll
       for (int wd = 0; wd < 4; ++wd) raw[wd] &= (int)vmask[wd];
     if constexpr (FP8) {
-      acc[nn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw[0], raw[1]), p[0], acc[nn], 0, 0, 0);
-      acc[nn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw[2], raw[3]), p[1], acc[nn], 0, 0, 0);
+      acc[nn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw[0], raw[1], vp2), p[0], acc[nn], 0, 0, 0);
+      acc[nn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp8x8_to_bf16(raw[2], raw[3], vp2), p[1], acc[nn], 0, 0, 0);
     } else {
       acc[nn] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, raw), p[0], acc[nn], 0, 0, 0);
     }
   }
 }
 
-template <bool FP8>
+template <bool FP8, bool WIN, bool BLK>
 __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a) {
   using GE = Geo<FP8>;
   constexpr int UB = GE::UB, UT = GE::UT, TILE = GE::TILE;
@@ -578,6 +659,10 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
   auto issue_at = [&](UnitRegs& R, int kt, int vt) __attribute__((always_inline)) {
     const char* kb = a.k + (size_t)kt * TILE;
     const char* vb = a.v + (size_t)vt * TILE;
+    if constexpr (BLK) {
+      R.ke = a.k_exp[kt];
+      R.ve = a.v_exp[vt];
+    }
 #pragma unroll
     for (int x = 0; x < 8; ++x) R.k[x] = __builtin_nontemporal_load((const i32x4*)(kb + kofs[x]));
 #pragma unroll
@@ -605,7 +690,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
     // operations complete in order) and no barrier holds it up (thirteen fp8
     // sequences of up to 5,395 tokens 20.2 -> 19.6 us; with two to four
     // sequences a lane nothing was left of it).
-    if constexpr (FP8) {
+    if constexpr (FP8 && !BLK) {
       for (int i = lane; i < Hkv; i += 64) {
         kscl[i] = a.k_scale[i];
         vscl[i] = a.v_scale[i];
@@ -614,7 +699,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
     int c = clamp_ctx(a.context_lens[min(lane, B - 1)], a.max_ctx);
     if (lane >= B) c = 0;
     issue_at(RA, ck, cv);
-    const int incl = wave_incl_scan(units_of<FP8>(c));
+    const int incl = wave_incl_scan(live_span<FP8, WIN>(a, c).nus);
     if (lane < B) {
       ctxs[lane] = c;
       pre[lane + 1] = incl;
@@ -624,7 +709,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
     __builtin_amdgcn_wave_barrier();
   } else {
     const int T = kWaves * 64, tid = threadIdx.x;
-    if constexpr (FP8) {
+    if constexpr (FP8 && !BLK) {
       for (int i = tid; i < Hkv; i += T) {
         kscl[i] = a.k_scale[i];
         vscl[i] = a.v_scale[i];
@@ -637,7 +722,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
       if (s < B) {
         const int c = clamp_ctx(a.context_lens[s], a.max_ctx);
         ctxs[s] = c;
-        local += units_of<FP8>(c);
+        local += live_span<FP8, WIN>(a, c).nus;
       }
     }
     issue_at(RA, ck, cv);
@@ -650,7 +735,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
       const int s = tid * per + k;
       if (s < B) {
         pre[s] = run;
-        run += units_of<FP8>(ctxs[s]);
+        run += live_span<FP8, WIN>(a, ctxs[s]).nus;
       }
     }
     if (tid == T - 1) pre[B] = run;
@@ -704,11 +789,10 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
         f_j = j;
       }
       const int nb = (ctxs[s] + kBlock - 1) / kBlock;
+      const Span sp = live_span<FP8, WIN>(a, ctxs[s]);
+      const int jr = real_unit<WIN>(sp, j);
       for (int b = 0; b < UB; ++b) {
-        // a block past the sequence's end is never fetched: its lanes re-read the
-        // unit's first block (same addresses as other lanes of the same load
-        // instruction, so no extra memory traffic) and its tokens are masked
-        const int blk = j * UB + (j * UB + b < nb ? b : 0);
+        const int blk = live_block<FP8, WIN>(a, sp, jr, b, nb);
         int id = a.block_tables[(size_t)s * a.max_blocks_per_seq + blk];
         id = id < 0 ? 0 : (id > a.num_blocks_m1 ? a.num_blocks_m1 : id);
         tiles[i * UB + b] = id * Hkv + g;
@@ -765,10 +849,11 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
 
     i32x4 qv[4];          // query group of the piece being computed
     i32x4 qE[4], qO[4];   // query groups of the segments of the next even / odd unit
-    float m_run = -INFINITY, l_part = 0.f, cscale = 0.f, vsc = 1.0f;
+    float m_run = kNoScore<WIN>, l_part = 0.f, cscale = 0.f, vsc = 1.0f;
     f32x4 acc[8];
     for (int nn = 0; nn < 8; ++nn) acc[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
     int piece_j0 = 0, ctx_s = 0;
+    Span sp{};
     bool piece_first = true;
 
     auto begin_piece = [&](int ui, const i32x4 (&qs)[4]) __attribute__((always_inline)) {
@@ -776,15 +861,16 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
         piece_first = ui == 0;
         piece_j0 = cs.j;
         ctx_s = __builtin_amdgcn_readfirstlane(ctxs[cs.s]);
+        if constexpr (WIN) sp = live_span<FP8, WIN>(a, ctx_s);
 #pragma unroll
         for (int c = 0; c < 4; ++c) qv[c] = qs[c];
         float ksc = 1.0f;
-        if constexpr (FP8) {
+        if constexpr (FP8 && !BLK) {
           ksc = kscl[cs.g];
           vsc = vscl[cs.g];
         }
         cscale = a.qk_scale_log2 * ksc;
-        m_run = -INFINITY;
+        m_run = kNoScore<WIN>;
         l_part = 0.f;
 #pragma unroll
         for (int nn = 0; nn < 8; ++nn) acc[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -792,14 +878,17 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
     };
 
     auto compute_unit = [&](const UnitRegs& R) __attribute__((always_inline)) {
-      attend_unit<FP8>(R, qv, cs.j * UT, ctx_s, lj, cscale, m_run, l_part, acc);
+      attend_unit<FP8, WIN, BLK>(R, qv, real_unit<WIN>(sp, cs.j) * UT, ctx_s, sp.lo, a.n_sink, lj, cscale, m_run,
+                                 l_part, acc);
     };
 
     // End of a piece: its rows (whole segment) or its partial record.
     auto finish_piece = [&](int ui) __attribute__((always_inline)) {
       const bool seg_end = cs.j == cs.nus - 1;
       if (!(seg_end || ui == n - 1)) return;
-      const float l_tot = xor_sum(l_part);
+      float l_tot = xor_sum(l_part);
+      // (no score but -infinity: zero sums, of a weight that any score outweighs)
+      if (WIN && l_tot == 0.f) l_tot = 1.0f;
       const float inv = vsc / l_tot;
       if (piece_j0 == 0 && seg_end) {  // the whole segment: final output, written straight out
         // (these stores follow the loads of the next unit, and a wait for any
@@ -1110,8 +1199,11 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
   }
 }
 
-template __global__ void paged_decode_kernel<false>(DecodeArgs);
-template __global__ void paged_decode_kernel<true>(DecodeArgs);
+template __global__ void paged_decode_kernel<false, false, false>(DecodeArgs);
+template __global__ void paged_decode_kernel<true, false, false>(DecodeArgs);
+template __global__ void paged_decode_kernel<false, true, false>(DecodeArgs);
+template __global__ void paged_decode_kernel<true, true, false>(DecodeArgs);
+template __global__ void paged_decode_kernel<true, true, true>(DecodeArgs);
 
 // Small calls: one workgroup per segment, no cut segments, no workspace.
 //
@@ -1133,7 +1225,7 @@ template __global__ void paged_decode_kernel<true>(DecodeArgs);
 constexpr int kSmallWaves = 8;
 constexpr int kSmallUnits = 2 * kSmallWaves;
 
-template <bool FP8>
+template <bool FP8, bool WIN, bool BLK>
 __global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(DecodeArgs a) {
   using GE = Geo<FP8>;
   constexpr int UB = GE::UB, UT = GE::UT, TILE = GE::TILE;
@@ -1153,19 +1245,30 @@ __global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(De
   // which are never read.  (Loading them ahead of the context length, unused,
   // saves 0.1 to 0.3 us of 8.6 to 11.0.)
   const int last = max((ctx + kBlock - 1) / kBlock - 1, 0);
+  const Span sp = live_span<FP8, WIN>(a, ctx);
   struct Entries { int ek, ev; };
   auto entries = [&](int u) __attribute__((always_inline)) {
+    if constexpr (WIN) {
+      const int j = real_unit<WIN>(sp, u);
+      return Entries{bt[live_block<FP8, WIN>(a, sp, j, kblk, last + 1)],
+                     bt[live_block<FP8, WIN>(a, sp, j, vblk, last + 1)]};
+    }
     return Entries{bt[min(u * UB + kblk, last)], bt[min(u * UB + vblk, last)]};
   };
   auto issue = [&](UnitRegs& R, const Entries& e) __attribute__((always_inline)) {
-    const char* kb = a.k + (size_t)(min(max(e.ek, 0), a.num_blocks_m1) * Hkv + g) * TILE;
-    const char* vb = a.v + (size_t)(min(max(e.ev, 0), a.num_blocks_m1) * Hkv + g) * TILE;
+    const int kt = min(max(e.ek, 0), a.num_blocks_m1) * Hkv + g, vt = min(max(e.ev, 0), a.num_blocks_m1) * Hkv + g;
+    const char* kb = a.k + (size_t)kt * TILE;
+    const char* vb = a.v + (size_t)vt * TILE;
+    if constexpr (BLK) {
+      R.ke = a.k_exp[kt];
+      R.ve = a.v_exp[vt];
+    }
 #pragma unroll
     for (int x = 0; x < 8; ++x) R.k[x] = __builtin_nontemporal_load((const i32x4*)(kb + kofs[x]));
 #pragma unroll
     for (int x = 0; x < 8; ++x) R.v[x] = __builtin_nontemporal_load((const i32x4*)(vb + vofs[x]));
   };
-  const int nus = units_of<FP8>(ctx);
+  const int nus = sp.nus;
   const bool two = w + kSmallWaves < nus;
   Entries e0{}, e1{};
   if (w < nus) {
@@ -1181,11 +1284,11 @@ __global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(De
       qv[c] = *(const i32x4*)(qrow + (FP8 ? 64 * (c >> 1) + 16 * lj + 8 * (c & 1) : 32 * c + 8 * lj));
   }
   float cscale = a.qk_scale_log2, vsc = 1.0f;
-  if constexpr (FP8) {
+  if constexpr (FP8 && !BLK) {
     cscale *= a.k_scale[g];
     vsc = a.v_scale[g];
   }
-  float m_run = -INFINITY, l_part = 0.f;
+  float m_run = kNoScore<WIN>, l_part = 0.f;
   f32x4 acc[8];
 #pragma unroll
   for (int nn = 0; nn < 8; ++nn) acc[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -1193,17 +1296,19 @@ __global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(De
     UnitRegs R0, R1;
     issue(R0, e0);
     issue(R1, e1);  // (without a second unit the first again, unused)
-    attend_unit<FP8>(R0, qv, w * UT, ctx, lj, cscale, m_run, l_part, acc);
+    attend_unit<FP8, WIN, BLK>(R0, qv, real_unit<WIN>(sp, w) * UT, ctx, sp.lo, a.n_sink, lj, cscale, m_run, l_part,
+                               acc);
     if (two) {
       // The second unit on a maximum of its own, as in slices of one unit: a
       // probability at its unit's maximum is 1 and not rounded (a running
       // maximum over both units: error against 64 bits 1.20e-3 of the norm,
       // 1.18e-3 this way, over four layers of up to 512 tokens).
-      float m1 = -INFINITY, l1 = 0.f;
+      float m1 = kNoScore<WIN>, l1 = 0.f;
       f32x4 acc1[8];
 #pragma unroll
       for (int nn = 0; nn < 8; ++nn) acc1[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
-      attend_unit<FP8>(R1, qv, (w + kSmallWaves) * UT, ctx, lj, cscale, m1, l1, acc1);
+      attend_unit<FP8, WIN, BLK>(R1, qv, real_unit<WIN>(sp, w + kSmallWaves) * UT, ctx, sp.lo, a.n_sink, lj, cscale, m1,
+                                 l1, acc1);
       const float M = fmaxf(m_run, m1);
       const float w0 = __builtin_amdgcn_exp2f(m_run - M), w1 = __builtin_amdgcn_exp2f(m1 - M);
       l_part = __builtin_fmaf(l1, w1, l_part * w0);
@@ -1244,7 +1349,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(De
         L = __builtin_fmaf(*(const float*)(rec[r] + 8192 + hd * 8 + 4), wgt, L);
       }
     }
-    o *= vsc / L;
+    if (!WIN || L != 0.f) o *= vsc / L;  // (scores of -infinity alone leave zeros)
   }
   const size_t off = ((size_t)s * a.hq + (size_t)g * G + hd) * kHeadDim + d0;
   if (a.out_fp32) {
@@ -1257,8 +1362,11 @@ __global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(De
   }
 }
 
-template __global__ void paged_decode_small_kernel<false>(DecodeArgs);
-template __global__ void paged_decode_small_kernel<true>(DecodeArgs);
+template __global__ void paged_decode_small_kernel<false, false, false>(DecodeArgs);
+template __global__ void paged_decode_small_kernel<true, false, false>(DecodeArgs);
+template __global__ void paged_decode_small_kernel<false, true, false>(DecodeArgs);
+template __global__ void paged_decode_small_kernel<true, true, false>(DecodeArgs);
+template __global__ void paged_decode_small_kernel<true, true, true>(DecodeArgs);
 
 // Zero n words (arrival counters).  A kernel rather than a memset, so that a
 // captured graph holds no memset node.
@@ -1300,18 +1408,30 @@ int device_cus(int* dev_out) {
   return cached[dev];
 }
 
+// The kernels of each cache type: without a window (bf16, e4m3), then with one
+// (bf16, e4m3, e4m3 with block scales).
+using Kernel = void (*)(DecodeArgs);
+constexpr int kVariants = 5;
+const Kernel kDecode[kVariants] = {paged_decode_kernel<false, false, false>, paged_decode_kernel<true, false, false>,
+                                   paged_decode_kernel<false, true, false>, paged_decode_kernel<true, true, false>,
+                                   paged_decode_kernel<true, true, true>};
+const Kernel kSmall[kVariants] = {
+    paged_decode_small_kernel<false, false, false>, paged_decode_small_kernel<true, false, false>,
+    paged_decode_small_kernel<false, true, false>, paged_decode_small_kernel<true, true, false>,
+    paged_decode_small_kernel<true, true, true>};
+
 // Workgroups of the kernel one compute unit holds at once (register-limited;
 // runtime occupancy query, cached).  Without a device: 1.
-int resident_per_cu(int dev, bool fp8) {
+int resident_per_cu(int dev, int variant) {
   static std::mutex mu;
-  static int cached[64][2] = {};
+  static int cached[64][kVariants] = {};
   if (dev < 0) return 1;
   std::lock_guard<std::mutex> lock(mu);
-  int& occ = cached[dev][fp8 ? 1 : 0];
+  int& occ = cached[dev][variant];
   if (!occ) {
     int n = 0;
-    const void* fn = fp8 ? (const void*)paged_decode_kernel<true> : (const void*)paged_decode_kernel<false>;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, fn, kWaves * 64, 0) != hipSuccess || n <= 0) {
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void*)kDecode[variant], kWaves * 64, 0) != hipSuccess ||
+        n <= 0) {
       (void)hipGetLastError();
       n = 1;
     }
@@ -1328,49 +1448,63 @@ struct Plan {
   size_t arrivals_off, rec_ml_off, rec_o_off, tile_cache_off, ws_bytes;
   int clear_words;  // arrival counters to zero before the launch (0 on the usual path)
   bool small;       // one workgroup per segment
+  int variant;      // index into kDecode and kSmall
+};
+
+struct Window {
+  int32_t window, n_sink;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-int validate(const dp_decode_shape* sh, Plan* plan) {
+// win: the window of window_decode_attention, null for paged_decode_attention
+int validate(const dp_decode_shape* sh, const Window* win, Plan* plan) {
   using dpool::fail;
-  if (!sh) return fail(DP_EINVAL, "paged_decode: null shape");
-  if (sh->head_dim != kHeadDim) return fail(DP_ENOTSUP, "paged_decode: head_dim %d (only 128)", sh->head_dim);
-  if (sh->block_size != kBlock) return fail(DP_ENOTSUP, "paged_decode: block_size %d (only 16)", sh->block_size);
-  if (sh->kv_dtype != DP_KV_BF16 && sh->kv_dtype != DP_KV_FP8_E4M3)
-    return fail(DP_ENOTSUP, "paged_decode: kv_dtype %d", sh->kv_dtype);
+  const char* const name = win ? "window_decode" : "paged_decode";
+  if (!sh) return fail(DP_EINVAL, "%s: null shape", name);
+  if (sh->head_dim != kHeadDim) return fail(DP_ENOTSUP, "%s: head_dim %d (only 128)", name, sh->head_dim);
+  if (sh->block_size != kBlock) return fail(DP_ENOTSUP, "%s: block_size %d (only 16)", name, sh->block_size);
+  if (sh->kv_dtype != DP_KV_BF16 && sh->kv_dtype != DP_KV_FP8_E4M3 && !(win && sh->kv_dtype == DP_KV_FP8_E4M3_BLOCK))
+    return fail(DP_ENOTSUP, "%s: kv_dtype %d", name, sh->kv_dtype);
   if (sh->out_dtype != DP_OUT_BF16 && sh->out_dtype != DP_OUT_FP32)
-    return fail(DP_ENOTSUP, "paged_decode: out_dtype %d", sh->out_dtype);
-  if (sh->reserved != 0) return fail(DP_EINVAL, "paged_decode: reserved must be 0");
-  if (sh->batch < 0) return fail(DP_EINVAL, "paged_decode: batch %d < 0", sh->batch);
+    return fail(DP_ENOTSUP, "%s: out_dtype %d", name, sh->out_dtype);
+  if (sh->reserved != 0) return fail(DP_EINVAL, "%s: reserved must be 0", name);
+  if (sh->batch < 0) return fail(DP_EINVAL, "%s: batch %d < 0", name, sh->batch);
   if (sh->batch > kMaxBatchInLds)
-    return fail(DP_ENOTSUP, "paged_decode: batch %d > %d sequences per call", sh->batch, kMaxBatchInLds);
+    return fail(DP_ENOTSUP, "%s: batch %d > %d sequences per call", name, sh->batch, kMaxBatchInLds);
   if (sh->n_q_heads <= 0 || sh->n_kv_heads <= 0 || sh->n_kv_heads > 65535 || sh->n_q_heads % sh->n_kv_heads)
-    return fail(DP_EINVAL, "paged_decode: n_q_heads %d must be a positive multiple of n_kv_heads %d",
-                sh->n_q_heads, sh->n_kv_heads);
+    return fail(DP_EINVAL, "%s: n_q_heads %d must be a positive multiple of n_kv_heads %d", name, sh->n_q_heads,
+                sh->n_kv_heads);
   if (sh->n_q_heads / sh->n_kv_heads > 16)
-    return fail(DP_ENOTSUP, "paged_decode: GQA group %d > 16", sh->n_q_heads / sh->n_kv_heads);
+    return fail(DP_ENOTSUP, "%s: GQA group %d > 16", name, sh->n_q_heads / sh->n_kv_heads);
   if (sh->max_blocks_per_seq <= 0 || sh->max_context_len < 0 ||
       (int64_t)sh->max_context_len > (int64_t)sh->max_blocks_per_seq * kBlock)
-    return fail(DP_EINVAL, "paged_decode: max_context_len %d must be in [0, 16 * max_blocks_per_seq = %lld]",
+    return fail(DP_EINVAL, "%s: max_context_len %d must be in [0, 16 * max_blocks_per_seq = %lld]", name,
                 sh->max_context_len, (long long)sh->max_blocks_per_seq * kBlock);
   if (sh->num_blocks <= 0 || sh->num_blocks * (int64_t)sh->n_kv_heads > INT32_MAX)
-    return fail(DP_EINVAL, "paged_decode: num_blocks %lld (num_blocks * n_kv_heads must fit int32)",
+    return fail(DP_EINVAL, "%s: num_blocks %lld (num_blocks * n_kv_heads must fit int32)", name,
                 (long long)sh->num_blocks);
-  const bool fp8 = sh->kv_dtype == DP_KV_FP8_E4M3;
+  if (win && (win->window < 1 || win->n_sink < 0))
+    return fail(DP_EINVAL, "%s: window %d must be at least 1, n_sink %d at least 0", name, win->window, win->n_sink);
+  const bool fp8 = sh->kv_dtype != DP_KV_BF16;
   const int unit = fp8 ? 64 : 32;
   const int P = sh->partition_tokens;
   if (P < 0 || P % unit || P / unit > kMaxUnitsPerWave)
-    return fail(DP_EINVAL, "paged_decode: partition_tokens %d must be a multiple of %d in [0, %d]", P, unit,
+    return fail(DP_EINVAL, "%s: partition_tokens %d must be a multiple of %d in [0, %d]", name, P, unit,
                 unit * kMaxUnitsPerWave);
   const int wpc = sh->workgroups_per_cu;
   if (wpc < 0 || wpc > kMaxWorkgroupsPerCu)
-    return fail(DP_EINVAL, "paged_decode: workgroups_per_cu %d outside [0, %d]", wpc, kMaxWorkgroupsPerCu);
-  const int64_t units_per_seq = ((int64_t)sh->max_context_len + unit - 1) / unit;
+    return fail(DP_EINVAL, "%s: workgroups_per_cu %d outside [0, %d]", name, wpc, kMaxWorkgroupsPerCu);
+  int64_t units_per_seq = ((int64_t)sh->max_context_len + unit - 1) / unit;
+  // (the units that the sinks hold, and the most that a window of that length touches)
+  if (win)
+    units_per_seq = std::min(units_per_seq, ((int64_t)win->n_sink + unit - 1) / unit +
+                                                ((int64_t)win->window + unit - 2) / unit + 1);
   const int64_t max_units = units_per_seq * sh->batch * sh->n_kv_heads;
-  if (max_units > INT32_MAX) return fail(DP_ENOTSUP, "paged_decode: %lld units exceed int32", (long long)max_units);
+  if (max_units > INT32_MAX) return fail(DP_ENOTSUP, "%s: %lld units exceed int32", name, (long long)max_units);
   plan->unit_tokens = unit;
   plan->min_chunk = P ? P / unit : 1;
+  plan->variant = win ? 2 + sh->kv_dtype : sh->kv_dtype;
   // LDS per workgroup: the kernel's static arrays (tile lists, wave sums,
   // each wave's two records, the workgroup's merge counters, with 256 bytes
   // for alignment) +
@@ -1379,10 +1513,10 @@ int validate(const dp_decode_shape* sh, Plan* plan) {
                       (size_t)kWaves * 2 * kRecBytes + (size_t)4 * kWaves * sizeof(int) + 256;
   plan->dyn_lds = (size_t)(2 * sh->batch + 1 + 2 * sh->n_kv_heads) * 4;
   if (stat + plan->dyn_lds > kLdsBytes)
-    return fail(DP_ENOTSUP, "paged_decode: %zu bytes of LDS per workgroup", stat + plan->dyn_lds);
+    return fail(DP_ENOTSUP, "%s: %zu bytes of LDS per workgroup", name, stat + plan->dyn_lds);
   int dev = -1;
   const int cus = device_cus(&dev);
-  const int per_cu = wpc ? std::min(wpc, resident_per_cu(dev, fp8)) : 1;
+  const int per_cu = wpc ? std::min(wpc, resident_per_cu(dev, plan->variant)) : 1;
   // persistent grid (every workgroup resident at once), grown only if some
   // slice would exceed kMaxUnitsPerWave, shrunk when slices would be shorter
   // than the minimum
@@ -1416,57 +1550,40 @@ int validate(const dp_decode_shape* sh, Plan* plan) {
   return DP_OK;
 }
 
-}  // namespace
-
-int dpool::decode_workspace_bytes(const dp_decode_shape* shape, size_t* bytes) {
-  Plan plan;
-  const int rc = validate(shape, &plan);
-  if (rc == DP_OK) *bytes = plan.ws_bytes;
-  return rc;
-}
-
-extern "C" size_t paged_decode_workspace_size(const dp_decode_shape* shape) {
-  size_t bytes = 0;
-  return dpool::decode_workspace_bytes(shape, &bytes) == DP_OK ? bytes : 0;
-}
-
-extern "C" int32_t paged_decode_partition_tokens(const dp_decode_shape* shape) {
-  Plan plan;
-  if (validate(shape, &plan) != DP_OK) return 0;
-  return plan.min_chunk * plan.unit_tokens;
-}
-
-extern "C" int paged_decode_attention(const void* q, const void* k_blocks, const void* v_blocks,
-                                      const int32_t* block_tables, const int32_t* context_lens, float scale,
-                                      const float* k_scale, const float* v_scale, void* out,
-                                      const dp_decode_shape* shape, void* workspace, size_t workspace_bytes,
-                                      void* stream) {
+int enqueue(const void* q, const void* k_blocks, const void* v_blocks, const int32_t* block_tables,
+            const int32_t* context_lens, float scale, const Window* win, const void* k_scale, const void* v_scale,
+            void* out, const dp_decode_shape* shape, void* workspace, size_t workspace_bytes, void* stream) {
   using dpool::fail;
+  const char* const name = win ? "window_decode" : "paged_decode";
   Plan plan;
-  int rc = validate(shape, &plan);
+  int rc = validate(shape, win, &plan);
   if (rc != DP_OK) return rc;
   if (shape->batch == 0) return DP_OK;
   if (!q || !k_blocks || !v_blocks || !block_tables || !context_lens || !out)
-    return fail(DP_EINVAL, "paged_decode: null tensor pointer");
-  const bool fp8 = shape->kv_dtype == DP_KV_FP8_E4M3;
-  if (fp8 && (!k_scale || !v_scale)) return fail(DP_EINVAL, "paged_decode: fp8 KV needs k_scale and v_scale");
-  if (!fp8 && (k_scale || v_scale)) return fail(DP_EINVAL, "paged_decode: k_scale/v_scale must be NULL for bf16 KV");
+    return fail(DP_EINVAL, "%s: null tensor pointer", name);
+  const bool fp8 = shape->kv_dtype != DP_KV_BF16;
+  if (fp8 && (!k_scale || !v_scale)) return fail(DP_EINVAL, "%s: fp8 KV needs k_scale and v_scale", name);
+  if (!fp8 && (k_scale || v_scale)) return fail(DP_EINVAL, "%s: k_scale/v_scale must be NULL for bf16 KV", name);
   if (((uintptr_t)q | (uintptr_t)k_blocks | (uintptr_t)v_blocks | (uintptr_t)out) & 15)
-    return fail(DP_EINVAL, "paged_decode: q, k_blocks, v_blocks and out must be 16-byte aligned");
+    return fail(DP_EINVAL, "%s: q, k_blocks, v_blocks and out must be 16-byte aligned", name);
   if (((uintptr_t)block_tables | (uintptr_t)context_lens) & 3)
-    return fail(DP_EINVAL, "paged_decode: block_tables and context_lens must be 4-byte aligned");
-  if (!std::isfinite(scale)) return fail(DP_EINVAL, "paged_decode: scale is not finite");
+    return fail(DP_EINVAL, "%s: block_tables and context_lens must be 4-byte aligned", name);
+  if (win && shape->kv_dtype == DP_KV_FP8_E4M3 && (((uintptr_t)k_scale | (uintptr_t)v_scale) & 3))
+    return fail(DP_EINVAL, "%s: k_scale and v_scale must be 4-byte aligned", name);
+  if (win && (out == q || out == workspace || q == workspace))
+    return fail(DP_EINVAL, "%s: q, out and workspace must not overlap", name);
+  if (!std::isfinite(scale)) return fail(DP_EINVAL, "%s: scale is not finite", name);
   if (!workspace || workspace_bytes < plan.ws_bytes)
-    return fail(DP_ENOMEM, "paged_decode: workspace needs %zu bytes, got %zu", plan.ws_bytes, workspace_bytes);
-  if ((uintptr_t)workspace & 255) return fail(DP_EINVAL, "paged_decode: workspace must be 256-byte aligned");
+    return fail(DP_ENOMEM, "%s: workspace needs %zu bytes, got %zu", name, plan.ws_bytes, workspace_bytes);
+  if ((uintptr_t)workspace & 255) return fail(DP_EINVAL, "%s: workspace must be 256-byte aligned", name);
   DecodeArgs a;
   a.q = (const uint16_t*)q;
   a.k = (const char*)k_blocks;
   a.v = (const char*)v_blocks;
   a.block_tables = block_tables;
   a.context_lens = context_lens;
-  a.k_scale = k_scale;
-  a.v_scale = v_scale;
+  a.k_scale = (const float*)k_scale;
+  a.v_scale = (const float*)v_scale;
   a.out = out;
   a.arrivals = (int32_t*)((char*)workspace + plan.arrivals_off);
   a.rec_ml = (float*)((char*)workspace + plan.rec_ml_off);
@@ -1482,24 +1599,67 @@ extern "C" int paged_decode_attention(const void* q, const void* k_blocks, const
   a.num_blocks_m1 = (int32_t)(shape->num_blocks - 1);
   a.out_fp32 = shape->out_dtype == DP_OUT_FP32;
   a.min_chunk = plan.min_chunk;
+  a.k_exp = (const uint8_t*)k_scale;
+  a.v_exp = (const uint8_t*)v_scale;
+  a.window = win ? std::min(win->window, std::max(a.max_ctx, 1)) : 0;
+  a.n_sink = win ? std::min(win->n_sink, a.max_ctx) : 0;
   (void)hipGetLastError();  // clear a stale error left by earlier work
   if (plan.small) {
-    hipLaunchKernelGGL(fp8 ? paged_decode_small_kernel<true> : paged_decode_small_kernel<false>,
-                       dim3(a.batch * a.hkv), dim3(kSmallWaves * 64), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL(kSmall[plan.variant], dim3(a.batch * a.hkv), dim3(kSmallWaves * 64), 0, (hipStream_t)stream, a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return fail(DP_EIO, "paged_decode: kernel launch failed: %s", hipGetErrorString(e));
+    if (e != hipSuccess) return fail(DP_EIO, "%s: kernel launch failed: %s", name, hipGetErrorString(e));
     return DP_OK;
   }
   if (plan.clear_words)
     hipLaunchKernelGGL(zero_words_kernel, dim3(std::min((plan.clear_words + 255) / 256, 1024)), dim3(256), 0,
                        (hipStream_t)stream, a.arrivals, plan.clear_words);
-  if (fp8)
-    hipLaunchKernelGGL(paged_decode_kernel<true>, dim3(plan.grid), dim3(kWaves * 64), plan.dyn_lds,
-                       (hipStream_t)stream, a);
-  else
-    hipLaunchKernelGGL(paged_decode_kernel<false>, dim3(plan.grid), dim3(kWaves * 64), plan.dyn_lds,
-                       (hipStream_t)stream, a);
+  hipLaunchKernelGGL(kDecode[plan.variant], dim3(plan.grid), dim3(kWaves * 64), plan.dyn_lds, (hipStream_t)stream, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(DP_EIO, "paged_decode: kernel launch failed: %s", hipGetErrorString(e));
+  if (e != hipSuccess) return fail(DP_EIO, "%s: kernel launch failed: %s", name, hipGetErrorString(e));
   return DP_OK;
+}
+
+}  // namespace
+
+int dpool::decode_workspace_bytes(const dp_decode_shape* shape, size_t* bytes) {
+  Plan plan;
+  const int rc = validate(shape, nullptr, &plan);
+  if (rc == DP_OK) *bytes = plan.ws_bytes;
+  return rc;
+}
+
+extern "C" size_t paged_decode_workspace_size(const dp_decode_shape* shape) {
+  size_t bytes = 0;
+  return dpool::decode_workspace_bytes(shape, &bytes) == DP_OK ? bytes : 0;
+}
+
+extern "C" int32_t paged_decode_partition_tokens(const dp_decode_shape* shape) {
+  Plan plan;
+  if (validate(shape, nullptr, &plan) != DP_OK) return 0;
+  return plan.min_chunk * plan.unit_tokens;
+}
+
+extern "C" int paged_decode_attention(const void* q, const void* k_blocks, const void* v_blocks,
+                                      const int32_t* block_tables, const int32_t* context_lens, float scale,
+                                      const float* k_scale, const float* v_scale, void* out,
+                                      const dp_decode_shape* shape, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
+  return enqueue(q, k_blocks, v_blocks, block_tables, context_lens, scale, nullptr, k_scale, v_scale, out, shape,
+                 workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t window_decode_workspace_size(const dp_decode_shape* shape, int32_t window, int32_t n_sink) {
+  const Window win{window, n_sink};
+  Plan plan;
+  return validate(shape, &win, &plan) == DP_OK ? plan.ws_bytes : 0;
+}
+
+extern "C" int window_decode_attention(const void* q, const void* k_blocks, const void* v_blocks,
+                                       const int32_t* block_tables, const int32_t* context_lens, float scale,
+                                       int32_t window, int32_t n_sink, const void* k_scale, const void* v_scale,
+                                       void* out, const dp_decode_shape* shape, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  const Window win{window, n_sink};
+  return enqueue(q, k_blocks, v_blocks, block_tables, context_lens, scale, &win, k_scale, v_scale, out, shape,
+                 workspace, workspace_bytes, stream);
 }

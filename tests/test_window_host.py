@@ -1,0 +1,63 @@
+"""Refusals of the window and block-scale operators (host side only: nothing is launched)."""
+import ctypes
+
+import pytest
+
+EINVAL, ENOMEM, ENOTSUP = -22, -12, -95
+P = 4096     # stands for any aligned device pointer; only calls that the host refuses get it
+
+
+def decode(lib, args=(), sh=(), window=64, n_sink=4, ws=1 << 30, **kw):
+    s = lib.decode_shape(**dict(dict(batch=4, n_q_heads=8, n_kv_heads=2, max_blocks_per_seq=100, max_context_len=1600,
+                                     num_blocks=500), **kw))
+    for k, v in dict(sh).items():
+        setattr(s, k, v)
+    fp8 = kw.get("kv_fp8") or kw.get("block_scales")
+    vals = dict(q=P, k=P, v=P, tables=P, ctx=P, scale=0.1, window=window, n_sink=n_sink, ks=P if fp8 else None,
+                vs=P if fp8 else None, out=2 * P)
+    vals.update(dict(args))
+    wsp = vals.pop("ws", 4 * P)
+    return lib.lib().window_decode_attention(*vals.values(), ctypes.byref(s), wsp, ws, None)
+
+
+@pytest.mark.parametrize("kw,sh,code", [
+    (dict(head_dim=64), {}, ENOTSUP), (dict(block_size=8), {}, ENOTSUP), ({}, dict(kv_dtype=3), ENOTSUP),
+    ({}, dict(kv_dtype=-1), ENOTSUP), ({}, dict(out_dtype=2), ENOTSUP), ({}, dict(reserved=1), EINVAL),
+    (dict(batch=-1), {}, EINVAL), (dict(batch=4097), {}, ENOTSUP), (dict(n_q_heads=7), {}, EINVAL),
+    (dict(n_q_heads=34), {}, ENOTSUP), (dict(max_context_len=1601), {}, EINVAL), (dict(num_blocks=0), {}, EINVAL),
+    (dict(window=0), {}, EINVAL), (dict(window=-5), {}, EINVAL), (dict(n_sink=-1), {}, EINVAL),
+    (dict(partition_tokens=48), {}, EINVAL), (dict(workgroups_per_cu=9), {}, EINVAL)])
+def test_decode_shapes_refused(host_lib, kw, sh, code):
+    assert decode(host_lib, sh=sh, **kw) == code
+    assert host_lib.last_error().startswith("window_decode")
+
+
+@pytest.mark.parametrize("args,kw", [
+    (dict(q=None), {}), (dict(k=None), {}), (dict(v=None), {}), (dict(tables=None), {}), (dict(ctx=None), {}),
+    (dict(out=None), {}), (dict(ks=P, vs=P), {}), (dict(ks=None), dict(kv_fp8=True)),
+    (dict(vs=None), dict(block_scales=True)), (dict(q=P + 8), {}), (dict(k=P + 4), {}), (dict(ctx=P + 2), {}),
+    (dict(ks=P + 2), dict(kv_fp8=True)), (dict(out=P), {}), (dict(out=4 * P), {}), (dict(q=4 * P), {}),
+    (dict(scale=float("nan")), {}), (dict(ws=4 * P + 16), {})])
+def test_decode_pointers_refused(host_lib, args, kw):
+    assert decode(host_lib, args, **kw) == EINVAL
+
+
+def test_decode_workspace(host_lib):
+    s = host_lib.decode_shape(4, 8, 2, 100, 1600, 500)
+    need = host_lib.window_workspace_size(s, 64, 4)
+    assert need > 0 and decode(host_lib, ws=need - 1) == ENOMEM and decode(host_lib, dict(ws=None)) == ENOMEM
+    assert host_lib.window_workspace_size(s, 0, 4) == 0 and host_lib.window_workspace_size(s, 64, -1) == 0
+    # never more than the whole context's, whatever the window and the sinks are
+    assert host_lib.window_workspace_size(s, 2 ** 31 - 1, 2 ** 31 - 1) <= host_lib.workspace_size(s)
+    with pytest.raises(host_lib.DpoolError):
+        host_lib.WindowDecoder(4, 8, 2, 100, 1600, 500, window=0, device="cpu")
+
+
+def test_empty_batch_is_fine(host_lib):
+    assert decode(host_lib, dict(q=None, k=None, v=None, out=None), batch=0) == 0
+
+
+def test_other_entry_points_refuse_block_scales(host_lib):
+    s = host_lib.decode_shape(4, 8, 2, 100, 1600, 500, block_scales=True)
+    assert s.kv_dtype == host_lib.KV_FP8_E4M3_BLOCK and host_lib.workspace_size(s) == 0
+    assert host_lib.lib().kv_cache_append(*[P] * 8, ctypes.byref(s), None) == ENOTSUP
