@@ -373,7 +373,7 @@ int paged_decode_attention_noalloc(const void* q, const void* k_blocks, const vo
 /* [n_kv_heads] and 4-byte aligned.  Calls whose windows and sinks hold few  */
 /* tokens count as short whatever max_context_len is.  q, out and workspace  */
 /* do not overlap (DP_EINVAL where they start together).  DP_EINVAL for      */
-/* window < 1 or n_sink < 0.                                                  */
+/* window < 1 or n_sink < 0; max_context_len <= 2^30.                         */
 /* ------------------------------------------------------------------------ */
 size_t window_decode_workspace_size(const dp_decode_shape* shape, int32_t window, int32_t n_sink);
 
@@ -469,6 +469,23 @@ int chunked_prefill_attention(const void* q, const void* k_blocks, const void* v
                               const int32_t* q_start, float scale, const float* k_scale,
                               const float* v_scale, void* out, const dp_prefill_shape* shape,
                               void* stream);
+
+/* Chunked prefill over a sliding window, and over block scales: row r at     */
+/* position p (as above) sees p - window < t <= p, and t < n_sink.  Window,   */
+/* sinks, kv_dtype DP_KV_FP8_E4M3_BLOCK and its k_scale and v_scale are as    */
+/* for window_decode_attention; everything else is as for                     */
+/* chunked_prefill_attention.  A row that sees only scores of -infinity gives */
+/* zeros.  Table entries of blocks that hold no token that some row sees are  */
+/* never read.  A cached V value that is not finite shows in the rows that    */
+/* see its token, and may show in rows up to 62 positions from those, in none */
+/* farther.  Supported: max_context_len <= 65536, or up to 2^30 where          */
+/* window + n_sink <= 65024.                                                   */
+/* q and out do not overlap (DP_EINVAL where they start together).            */
+int window_prefill_attention(const void* q, const void* k_blocks, const void* v_blocks,
+                             const int32_t* block_tables, const int32_t* context_lens,
+                             const int32_t* q_start, float scale, int32_t window, int32_t n_sink,
+                             const void* k_scale, const void* v_scale, void* out,
+                             const dp_prefill_shape* shape, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Block tables and slot maps on the device (asynchronous).                  */

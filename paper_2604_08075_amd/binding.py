@@ -34,7 +34,7 @@ EXPORTS = (
     "route_adapt_default_params", "route_adapt_threshold", "dp_cost_model",
     "paged_decode_workspace_size", "paged_decode_partition_tokens", "paged_decode_attention",
     "paged_decode_attention_noalloc", "window_decode_workspace_size", "window_decode_attention",
-    "kv_cache_append", "chunked_prefill_attention", "kv_tables_step", "qk_norm_rope_append",
+    "kv_cache_append", "chunked_prefill_attention", "window_prefill_attention", "kv_tables_step", "qk_norm_rope_append",
     "tree_decode_workspace_size", "tree_decode_attention", "kv_cache_accept", "dp_hbm_read_probe",
 )
 
@@ -165,6 +165,8 @@ def lib() -> ctypes.CDLL:
         L.kv_cache_append.argtypes = [ctypes.c_void_p] * 8 + [ctypes.POINTER(DecodeShape), ctypes.c_void_p]
         L.chunked_prefill_attention.argtypes = [ctypes.c_void_p] * 6 + [ctypes.c_float] + [ctypes.c_void_p] * 3 + [
             ctypes.POINTER(PrefillShape), ctypes.c_void_p]
+        L.window_prefill_attention.argtypes = [ctypes.c_void_p] * 6 + [ctypes.c_float] + [ctypes.c_int32] * 2 + [
+            ctypes.c_void_p] * 3 + [ctypes.POINTER(PrefillShape), ctypes.c_void_p]
         L.kv_tables_step.argtypes = [ctypes.c_void_p] * 15 + [ctypes.POINTER(TablesShape), ctypes.c_void_p]
         L.qk_norm_rope_append.argtypes = [ctypes.c_void_p] * 5 + [ctypes.c_float] + [ctypes.c_void_p] * 8 + [
             ctypes.POINTER(QKShape), ctypes.c_void_p]
@@ -410,9 +412,11 @@ def kv_cache_append(k_new, v_new, k_blocks, v_blocks, block_tables, positions, s
 
 
 def prefill_shape(batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks, total_q,
-                  kv_fp8=False, out_fp32=False, query_tile=0, head_dim=128, block_size=16) -> PrefillShape:
+                  kv_fp8=False, out_fp32=False, query_tile=0, head_dim=128, block_size=16,
+                  block_scales=False) -> PrefillShape:
+    """block_scales: an e4m3 cache with a scale for each block and head (window_prefill_attention)."""
     return PrefillShape(batch, n_q_heads, n_kv_heads, head_dim, block_size, max_blocks_per_seq, max_context_len,
-                        KV_FP8_E4M3 if kv_fp8 else KV_BF16, OUT_FP32 if out_fp32 else OUT_BF16, query_tile, 0,
+                        _kv_dtype(kv_fp8, block_scales), OUT_FP32 if out_fp32 else OUT_BF16, query_tile, 0,
                         total_q, num_blocks)
 
 
@@ -422,6 +426,17 @@ def chunked_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens,
     check(lib().chunked_prefill_attention(
         q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
         q_start.data_ptr(), float(scale), k_scale.data_ptr() if k_scale is not None else None,
+        v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape),
+        _stream_ptr(stream)))
+
+
+def window_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens, q_start, scale, window, n_sink, out,
+                             shape: PrefillShape, k_scale=None, v_scale=None, stream=None) -> None:
+    """Enqueue the chunked prefill over a sliding window and the first n_sink tokens, or over block scales
+    (include/dpool.h, window_prefill_attention)."""
+    check(lib().window_prefill_attention(
+        q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
+        q_start.data_ptr(), float(scale), window, n_sink, k_scale.data_ptr() if k_scale is not None else None,
         v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape),
         _stream_ptr(stream)))
 

@@ -1451,6 +1451,8 @@ struct Plan {
   int variant;      // index into kDecode and kSmall
 };
 
+constexpr int kMaxWindowContext = 1 << 30;  // positions, and a little above, are 32-bit
+
 struct Window {
   int32_t window, n_sink;
 };
@@ -1486,6 +1488,8 @@ int validate(const dp_decode_shape* sh, const Window* win, Plan* plan) {
                 (long long)sh->num_blocks);
   if (win && (win->window < 1 || win->n_sink < 0))
     return fail(DP_EINVAL, "%s: window %d must be at least 1, n_sink %d at least 0", name, win->window, win->n_sink);
+  if (win && sh->max_context_len > kMaxWindowContext)
+    return fail(DP_ENOTSUP, "%s: max_context_len above %d", name, kMaxWindowContext);
   const bool fp8 = sh->kv_dtype != DP_KV_BF16;
   const int unit = fp8 ? 64 : 32;
   const int P = sh->partition_tokens;

@@ -60,6 +60,20 @@
 // start in distinct banks, and every operand is a constant away from one base.
 // Tokens at or past T inside the last tile are zero in LDS (their V could be
 // stale or poisoned; zero keeps 0 * V finite) and masked by causality.
+//
+// Windows (WIN): a row at position p sees p - window < t <= p and t < n_sink.
+// An item's steps are then those with a token that one of its rows sees, the
+// sinks' before the window's; `real` turns a step into its place in the
+// context, and the block ids staged in LDS are those steps' (so that a context
+// may be longer than kIdCap blocks where its window is not).  The steps at the
+// window's edge go through the masking branch, as those at the diagonal do.
+// Tokens of an item's tiles that none of its rows sees are zero in LDS, and a
+// wave takes the V operands of a tile that its own rows do not see from a block
+// of zeros: what is there need not be finite.
+//
+// Block scales (BLK): the copy of a piece multiplies by 2^(e - 127) where it
+// widens e4m3 to bf16, in the same instruction; e is one byte per 2 KiB tile,
+// loaded with the piece.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -88,6 +102,9 @@ constexpr float kMinusBig = -3.0e38f; // the reference max of a column with no s
 constexpr int kMaxBatch = 4096;
 constexpr int kIdCap = 4096;          // block ids staged in LDS: contexts up to 65,536 tokens
 constexpr int kList = 64;             // rounds of items looked up at once
+constexpr int kMaxPairBatch = 3968;         // (160 KiB less 97.8 KiB) over 16 bytes a sequence, rounded down
+constexpr int kMaxWindowContext = 1 << 30;  // positions, and a little above, are 32-bit
+constexpr int kWindowRoom = 512;      // tokens of an item's steps beside window and sinks: 255 + 3 * 63, rounded up
 // LDS layout of a sub-tile (byte offsets; a chunk is 16 bytes)
 constexpr int kKPitch = 320, kKSlot = 32 * kKPitch + 32;
 constexpr int kVPitch = 64, kVSlot = 128 * kVPitch + 512;
@@ -108,6 +125,9 @@ struct PrefillArgs {
   int32_t batch, hq, hkv, group;
   int32_t max_blocks_per_seq, max_ctx, num_blocks_m1, out_fp32;
   int32_t total_q;
+  const uint8_t* k_exp;         // [num_blocks, Hkv] exponent bytes (BLK)
+  const uint8_t* v_exp;
+  int32_t window, n_sink;       // (WIN; both at most max_ctx)
 };
 
 // Max over the four lanes li, li + 16, li + 32, li + 48
@@ -145,11 +165,12 @@ __device__ __forceinline__ int wave_max(int x) {
   return __builtin_amdgcn_readlane(x, 63);
 }
 
-__device__ __forceinline__ i32x4 fp8x8_to_bf16(int lo, int hi) {
-  bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-  bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-  bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+// Eight e4m3 bytes times a power of two.
+__device__ __forceinline__ i32x4 fp8x8_to_bf16(int lo, int hi, float pow2 = 1.0f) {
+  bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, pow2, false);
+  bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, pow2, true);
+  bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, pow2, false);
+  bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, pow2, true);
   return i32x4{__builtin_bit_cast(int, a), __builtin_bit_cast(int, b), __builtin_bit_cast(int, c),
                __builtin_bit_cast(int, d)};
 }
@@ -176,7 +197,7 @@ __device__ __forceinline__ void lds_barrier() {
 // A workgroup of kWaves waves, each with NC blocks of 16 columns.  S: the
 // waves are S to a column group and take turns at its sub-tiles; their sums
 // are folded through LDS at the end of the item.
-template <bool FP8, int kWaves, int NC, int S>
+template <bool FP8, int kWaves, int NC, int S, bool WIN, bool BLK>
 __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) {
   constexpr int kThreads = kWaves * 64;
   constexpr int kWaveCols = 16 * NC;            // (token, head) columns of a wave
@@ -192,6 +213,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
   __shared__ int wsum[kWaves];
   __shared__ int list[kList][2];  // (sequence, tile) of this workgroup's next rounds
   __shared__ float first_max[kWaves / S][NC][16];  // S > 1: the columns' first reference maxima
+  // V operands of a tile that a wave's rows do not see (WIN): all its reads, from one base
+  constexpr int kZeros = WIN ? 3 * (32 * kVPitch + 128) + 4 * kVPitch + 16 : 16;
+  __shared__ __attribute__((aligned(16))) char zero_v[kZeros];
   extern __shared__ int tile_pre[];  // [B + 1] items per KV head of sequences 0..s-1, then r0[B], r1[B], T[B]
 
   const int tid = threadIdx.x;
@@ -204,6 +228,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
   int* const row1 = row0 + B;
   int* const ctx = row1 + B;
 
+  if constexpr (WIN)
+    for (int i = tid; i < kZeros / 16; i += kThreads) *(i32x4*)(zero_v + 16 * i) = i32x4{0, 0, 0, 0};
   if (tid == 0) tile_pre[0] = 0;
   for (int base = 0; base < B; base += kThreads) {
     __syncthreads();
@@ -326,7 +352,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     const int c0 = qt * COLS;
     const int tok_last = (min(c0 + COLS, ncols) - 1) / G;
     const int n_kv = T - n + tok_last + 1;
-    const int nt = (n_kv + ST - 1) / ST;
+    // With a window, steps `head` .. are those from head + gap on of the context:
+    // the steps between hold no token that a row of the item sees.
+    const int lo = WIN ? max(T - n + c0 / G - a.window + 1, 0) : 0;  // the item's first token, sinks aside
+    const int head = WIN ? min((a.n_sink + ST - 1) / ST, lo / ST) : 0;
+    const int gap = WIN ? lo / ST - head : 0;
+    auto real = [&](int j) __attribute__((always_inline)) { return WIN && j >= head ? j + gap : j; };
+    // the first step of the item at or past step r of the context
+    auto from = [&](int r) __attribute__((always_inline)) { return !WIN || r <= head ? r : max(r - gap, head); };
+    const int nt = (n_kv + ST - 1) / ST - gap;
     const int nb = (T + kBS - 1) / kBS;
     const int32_t* bt = a.block_tables + (size_t)s * a.max_blocks_per_seq;
     const int pmin = T - n + min(c0 + cg * kWaveCols, ncols - 1) / G;  // first position of this wave's columns
@@ -334,15 +368,38 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     // not of the item's, and none without a column.  Past them every one of
     // its probabilities is 0, and 0 times a value that is not finite is not.
     const int p_end = T - n + (min(c0 + (cg + 1) * kWaveCols, ncols) - 1) / G;
-    const int nt_w = c0 + cg * kWaveCols >= ncols || p_end < kKT * ks ? 0 : (p_end - kKT * ks) / ST + 1;
+    const int nt_w = c0 + cg * kWaveCols >= ncols || p_end < kKT * ks ? 0 : from((p_end - kKT * ks) / ST + 1);
+    // (WIN) the first and the last column's window begin here
+    const int lo_first = pmin - a.window + 1, lo_last = p_end - a.window + 1;
+    // the wave sees nothing of step j
+    auto hidden = [&](int j) __attribute__((always_inline)) {
+      const int t0 = ST * real(j) + kKT * ks;
+      return WIN && t0 + kKT <= lo_first && t0 >= a.n_sink;
+    };
 
     float cmul = a.scale_log2, vsc = 1.0f;
-    if constexpr (FP8) {
+    int q_sign = 0;
+    if constexpr (FP8 && !BLK) {
       cmul *= a.k_scale[g];
       vsc = a.v_scale[g];
+      if constexpr (WIN) {
+        // Masks and reference maxima need a factor above 0: a scale below it
+        // turns the queries' signs, and a scale of 0 makes all scores as good
+        // as equal.
+        if (cmul < 0.f) q_sign = (int)0x80008000u;
+        cmul = cmul == 0.f ? 1e-30f : fabsf(cmul);
+        cmul = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(cmul)));
+      }
     }
-    const int n_ids = min(min(2 * S * nt, nb), kIdCap);
-    const int id0 = bt[min(tid, n_ids - 1)];  // the first ids' loads go out before the queries'
+    // Block id i of the item's steps.  A block that no row of the item sees
+    // (its entry may be anything) is stood for by the window's first.
+    auto entry = [&](int i) __attribute__((always_inline)) {
+      if constexpr (!WIN) return i;
+      const int b = i >= 2 * S * head ? i + 2 * S * gap : i;
+      return b * kBS >= a.n_sink && b * kBS + kBS <= lo ? lo / kBS : b;
+    };
+    const int n_ids = min(min(2 * S * nt, nb - 2 * S * gap), kIdCap);
+    const int id0 = bt[entry(min(tid, n_ids - 1))];  // the first ids' loads go out before the queries'
     // token of the chunk and row (token, head) of this lane's column in block b; idle columns repeat the last one
     auto column = [&](int b, int& tok, size_t& row) __attribute__((always_inline)) {
       const int cc = min(c0 + cg * kWaveCols + 16 * b + li, ncols - 1);
@@ -359,15 +416,21 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
       pcol[b] = T - n + tok;
       const uint16_t* qp = a.q + row * kD + 8 * lj;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) qf[b][c] = *(const i32x4*)(qp + 32 * c);
+      for (int c = 0; c < 4; ++c) {
+        qf[b][c] = *(const i32x4*)(qp + 32 * c);
+        if constexpr (WIN && FP8 && !BLK) qf[b][c] ^= i32x4{q_sign, q_sign, q_sign, q_sign};
+      }
     }
     if (tid < n_ids) ids_lds[tid] = min(max(id0, 0), a.num_blocks_m1);
-    for (int i = tid + kThreads; i < n_ids; i += kThreads) ids_lds[i] = min(max(bt[i], 0), a.num_blocks_m1);
+    for (int i = tid + kThreads; i < n_ids; i += kThreads) ids_lds[i] = min(max(bt[entry(i)], 0), a.num_blocks_m1);
     lds_barrier();
 
     constexpr int TB = FP8 ? 2048 : 4096;
     struct Ids { int x[S]; };
-    struct Chunk { Piece x[S * NL]; };
+    struct Chunk {
+      Piece x[S * NL];
+      int e[S];  // exponent bytes of the pieces' tiles (BLK)
+    };
     auto read_ids = [&](int j, Ids& id) __attribute__((always_inline)) {
 #pragma unroll
       for (int x = 0; x < S; ++x) id.x[x] = ids_lds[min(2 * (S * j + x) + cb, n_ids - 1)];
@@ -376,30 +439,58 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
 #pragma unroll
       for (int x = 0; x < S; ++x) t.x[x] = __builtin_amdgcn_readfirstlane(id.x[x]) * a.hkv + g;
     };
-    auto load = [&](const char* base, int off, const Ids& t, Chunk& r) __attribute__((always_inline)) {
+    auto load = [&](const char* base, const uint8_t* exps, int off, const Ids& t, Chunk& r)
+                    __attribute__((always_inline)) {
 #pragma unroll
       for (int x = 0; x < S; ++x) {
+        if constexpr (BLK) r.e[x] = exps[t.x[x]];
         const char* p = base + (size_t)t.x[x] * TB + off;
 #pragma unroll
         for (int y = 0; y < NL; ++y) r.x[x * NL + y] = *(const Piece*)(p + 512 * EB * y);
       }
     };
-    auto widen = [&](const Piece& p) __attribute__((always_inline)) {
-      if constexpr (FP8) return fp8x8_to_bf16(p[0], p[1]);
+    auto widen = [&](const Chunk& r, int x) __attribute__((always_inline)) {
+      const Piece& p = r.x[x];
+      if constexpr (BLK) return fp8x8_to_bf16(p[0], p[1], __uint_as_float((unsigned)r.e[x / NL] << 23));
+      else if constexpr (FP8) return fp8x8_to_bf16(p[0], p[1]);
       else return p;
     };
     auto store_k = [&](int slot, int x, const Chunk& r) __attribute__((always_inline)) {
-      *(i32x4*)(tiles.k[slot][x / NL] + kdst + 4 * kKPitch * (x % NL)) = widen(r.x[x]);
+      *(i32x4*)(tiles.k[slot][x / NL] + kdst + 4 * kKPitch * (x % NL)) = widen(r, x);
     };
     auto store_v = [&](int slot, int x, const Chunk& r) __attribute__((always_inline)) {
-      *(i32x4*)(tiles.v[slot][x / NL] + vdst + (32 * kVPitch + 128) * (x % NL)) = widen(r.x[x]);
+      *(i32x4*)(tiles.v[slot][x / NL] + vdst + (32 * kVPitch + 128) * (x % NL)) = widen(r, x);
     };
-    // zero the tokens of V tile j past the sequence's end
-    auto clip_v = [&](int j, Chunk& r) __attribute__((always_inline)) {
+    // zero the tokens of V tile j past the sequence's end (and those that no row of the item sees)
+    auto clip_v = [&](int j0, Chunk& r) __attribute__((always_inline)) {
+      const int j = real(j0);
+      if (WIN && ST * j < lo && ST * j + ST > a.n_sink) {
+#pragma unroll
+        for (int x = 0; x < S * NL; ++x) {
+          const int t0 = ST * j + kKT * (x / NL) + 16 * cb + 8 * (lane & 1);
+          auto before = [&](int t) __attribute__((always_inline)) { return (1u << min(max(t - t0, 0), 8)) - 1; };
+          const unsigned live = ~before(lo) | before(a.n_sink);  // a bit for each of the eight tokens
+          if constexpr (BLK) {
+            // (a scale of NaN would make NaN of the zeros: no token of the block is seen)
+            if ((t0 & ~15) >= a.n_sink && (t0 & ~15) + kBS <= lo) r.e[x / NL] = 0;
+          }
+#pragma unroll
+          for (int wd = 0; wd < (FP8 ? 2 : 4); ++wd) {
+            unsigned m = 0;
+#pragma unroll
+            for (int y = 0; y < (FP8 ? 4 : 2); ++y)
+              if ((live >> ((FP8 ? 4 : 2) * wd + y)) & 1) m |= FP8 ? 0xffu << (8 * y) : 0xffffu << (16 * y);
+            r.x[x][wd] &= (int)m;
+          }
+        }
+      }
       if (ST * j + ST > T) {
 #pragma unroll
         for (int x = 0; x < S * NL; ++x) {
           const int t0 = ST * j + kKT * (x / NL) + 16 * cb + 8 * (lane & 1);
+          if constexpr (BLK && WIN) {
+            if ((t0 & ~15) >= T) r.e[x / NL] = 0;  // (a block past the end: another's stands for it)
+          }
           if constexpr (FP8) {
 #pragma unroll
             for (int wd = 0; wd < 2; ++wd) {
@@ -441,12 +532,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
       tb[0] = t[2];
       tb[1] = t[3];
       Chunk k0, k1;
-      load(a.k, koff_g, t[0], k0);
-      load(a.k, koff_g, t[1], k1);
-      load(a.k, koff_g, t[2], kA);
-      load(a.v, voff_g, t[0], vA);
-      load(a.k, koff_g, t[3], kB);
-      load(a.v, voff_g, t[1], vB);
+      load(a.k, a.k_exp, koff_g, t[0], k0);
+      load(a.k, a.k_exp, koff_g, t[1], k1);
+      load(a.k, a.k_exp, koff_g, t[2], kA);
+      load(a.v, a.v_exp, voff_g, t[0], vA);
+      load(a.k, a.k_exp, koff_g, t[3], kB);
+      load(a.v, a.v_exp, voff_g, t[1], vB);
 #pragma unroll
       for (int y = 0; y < S * NL; ++y) {
         store_k(0, y, k0);
@@ -458,9 +549,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     auto kfrag = [&](int slot, int f) __attribute__((always_inline)) {  // f = 4 m + c
       return *(const i32x4*)(tiles.k[slot][ks] + kro + 4 * kKPitch * (f >> 2) + 64 * (f & 3));
     };
-    auto vfrag = [&](int slot, int nn) __attribute__((always_inline)) {
-      return *(const i32x4*)(tiles.v[slot][ks] + vro + (32 * kVPitch + 128) * (nn >> 1) + 4 * kVPitch * (nn & 1));
+    auto vbase = [&](int slot) __attribute__((always_inline)) { return (const char*)tiles.v[slot][ks] + vro; };
+    auto vread = [&](const char* base, int nn) __attribute__((always_inline)) {
+      return *(const i32x4*)(base + (32 * kVPitch + 128) * (nn >> 1) + 4 * kVPitch * (nn & 1));
     };
+    auto vfrag = [&](int slot, int nn) __attribute__((always_inline)) { return vread(vbase(slot), nn); };
     struct Scores { f32x4 z[NC][2]; };       // [column block][m]: tokens 8 lj + 4 m + e
     struct Probs { i32x4 p[NC]; };
     // S^T += K Q^T: row group and 32-dim chunk f, column block b
@@ -493,13 +586,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     // the rare work ahead of step j: causal masking, and moving the reference
     // maxima; true if the sums so far must be rescaled by alpha
     auto prepare = [&](int j, Scores& sc) __attribute__((always_inline)) {
-      const int t0 = ST * j + kKT * ks;
-      if (t0 + kKT - 1 > pmin) {
+      const int t0 = ST * real(j) + kKT * ks;
+      if (t0 + kKT - 1 > pmin || (WIN && t0 < lo_last && t0 + kKT > a.n_sink)) {
 #pragma unroll
         for (int b = 0; b < NC; ++b) {
+          const int hid0 = WIN ? a.n_sink - t0 - 8 * lj : 0;                    // the column's hidden tokens:
+          const int hid1 = WIN ? pcol[b] - a.window + 1 - t0 - 8 * lj : 0;      // x in [hid0, hid1)
 #pragma unroll
           for (int x = 0; x < 8; ++x)
-            if (t0 + 8 * lj + x > pcol[b]) sc.z[b][x >> 2][x & 3] = -INFINITY;
+            if (t0 + 8 * lj + x > pcol[b] || (WIN && x >= hid0 && x < hid1)) sc.z[b][x >> 2][x & 3] = -INFINITY;
 #pragma unroll
           for (int y = 0; y < 4; ++y) colmax(sc, b, y);
         }
@@ -565,7 +660,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     for (int b = 0; b < NC; ++b) pB.p[b] = i32x4{0, 0, 0, 0};
     // first step with a token past some column's position in its scores, or
     // past the sequence's end in the V tile it writes
-    const int j_rare = min((pmin + 1 - kKT * ks) / ST, T / ST);
+    const int j_rare = from(min((pmin + 1 - kKT * ks) / ST, T / ST));
+    // (WIN) steps before this one may hold tokens that some column's window has passed
+    const int j_left = WIN ? from((max(lo_last, 0) + ST - 1) / ST) : 0;
     // One step: scores of tile j+1, output products of tile j-1 and
     // probabilities of tile j, independent of one another, in sixteen slots
     // of four matrix products each.
@@ -573,8 +670,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
                     __attribute__((always_inline)) {
 #pragma unroll
       for (int f = 0; f < 4; ++f) kf[f] = kfrag(par ^ 1, f);
+      const char* const vb = hidden(j - 1) ? (const char*)zero_v : vbase(par ^ 1);
       bool grown = false;
-      if (j >= j_rare || __builtin_amdgcn_ballot_w64(over > 0.f) != 0) {
+      if (j >= j_rare || (WIN && j < j_left) || __builtin_amdgcn_ballot_w64(over > 0.f) != 0) {
         grown = prepare(j, cur);
         clip_v(j, vr);
       }
@@ -622,7 +720,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
         // operand reads, four slots ahead
         if (b == NC - 1) {
           if (i < 4) kf[i + 4] = kfrag(par ^ 1, i + 4);
-          else if (i < 12) vf[i - 4] = vfrag(par ^ 1, i - 4);
+          else if (i < 12) vf[i - 4] = vread(vb, i - 4);
         }
         // column maxima of the next scores, well after the products that made them
 #pragma unroll
@@ -637,8 +735,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
           if (i == 0) bases(idn, t4);
           if (i < NS) store_k(par, i, kr);
           else if (i < 2 * NS) store_v(par, i - NS, vr);
-          else if (i == 2 * NS) load(a.k, koff_g, t4, kr);
-          else if (i == 2 * NS + 1) load(a.v, voff_g, tb[0], vr);
+          else if (i == 2 * NS) load(a.k, a.k_exp, koff_g, t4, kr);
+          else if (i == 2 * NS + 1) load(a.v, a.v_exp, voff_g, tb[0], vr);
           else if (i == 10) {
             tb[0] = tb[1];
             tb[1] = t4;
@@ -698,8 +796,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
         store_k(par, x, kr);
         store_v(par, x, vr);
       }
-      load(a.k, koff_g, t4, kr);
-      load(a.v, voff_g, tb[0], vr);
+      load(a.k, a.k_exp, koff_g, t4, kr);
+      load(a.v, a.v_exp, voff_g, tb[0], vr);
       tb[0] = tb[1];
       tb[1] = t4;
       read_ids(j + 5, idn);
@@ -748,7 +846,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     if constexpr (S == 1) {
 #pragma unroll
       for (int b = 0; b < NC; ++b)
-        store_row(b, 0, std::integral_constant<int, 8>{}, vsc / lsum[b][0],
+        store_row(b, 0, std::integral_constant<int, 8>{}, WIN && lsum[b][0] == 0.f ? 0.f : vsc / lsum[b][0],
                     [&](int nn) __attribute__((always_inline)) { return acc[b][nn]; });
     } else {
       // Fold the two halves of the KV range: each wave of a pair hands the
@@ -779,7 +877,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
         const float om = ml[((ow * NC + b) * 64 + lane) * 2], ol = ml[((ow * NC + b) * 64 + lane) * 2 + 1];
         const float mx = fmaxf(mc[b], om);
         const float w0 = __builtin_amdgcn_exp2f(mc[b] - mx), w1 = __builtin_amdgcn_exp2f(om - mx);
-        const float inv = vsc / __builtin_fmaf(ol, w1, lsum[b][0] * w0);
+        const float den = __builtin_fmaf(ol, w1, lsum[b][0] * w0);
+        const float inv = WIN && den == 0.f ? 0.f : vsc / den;  // (scores of -infinity alone leave zeros)
         store_row(b, 4 * ks, std::integral_constant<int, 4>{}, inv, [&](int nn) __attribute__((always_inline)) {
             const f32x4 x = part[((ow * NC + b) * 4 + nn) * 64 + lane];
             const f32x4 y = pick(acc[b][nn], acc[b][4 + nn]);
@@ -820,61 +919,86 @@ int compute_units() {
   return cached[dev];
 }
 
+// The cache types, without and with a window.
+enum Cache { kBf16, kFp8, kWinBf16, kWinFp8, kWinBlock };
+
+struct Window {
+  int32_t window, n_sink;
+};
+
 // Enqueue one variant: as many persistent workgroups as the device holds, or
 // one per item (an upper bound; the kernel counts them exactly).
 template <int kWaves, int NC, int S>
-void launch(const PrefillArgs& a, bool fp8, int64_t workgroups, hipStream_t st) {
+void launch(const PrefillArgs& a, Cache cache, int64_t workgroups, hipStream_t st) {
   constexpr int cols = 16 * NC * kWaves / S;
   const int64_t items = (((int64_t)a.total_q * a.group + cols - 1) / cols + a.batch) * a.hkv;
   const dim3 grid((unsigned)std::min(items, workgroups)), block(kWaves * 64);
   const size_t dyn = (size_t)(4 * a.batch + 1) * sizeof(int);  // tile prefix, rows, contexts
-  if (fp8) hipLaunchKernelGGL((prefill_kernel<true, kWaves, NC, S>), grid, block, dyn, st, a);
-  else hipLaunchKernelGGL((prefill_kernel<false, kWaves, NC, S>), grid, block, dyn, st, a);
+  switch (cache) {
+    case kBf16: hipLaunchKernelGGL((prefill_kernel<false, kWaves, NC, S, false, false>), grid, block, dyn, st, a); break;
+    case kFp8: hipLaunchKernelGGL((prefill_kernel<true, kWaves, NC, S, false, false>), grid, block, dyn, st, a); break;
+    case kWinBf16:
+      hipLaunchKernelGGL((prefill_kernel<false, kWaves, NC, S, true, false>), grid, block, dyn, st, a);
+      break;
+    case kWinFp8: hipLaunchKernelGGL((prefill_kernel<true, kWaves, NC, S, true, false>), grid, block, dyn, st, a); break;
+    case kWinBlock: hipLaunchKernelGGL((prefill_kernel<true, kWaves, NC, S, true, true>), grid, block, dyn, st, a); break;
+  }
 }
 
-}  // namespace
-
-extern "C" int chunked_prefill_attention(const void* q, const void* k_blocks, const void* v_blocks,
-                                         const int32_t* block_tables, const int32_t* context_lens,
-                                         const int32_t* q_start, float scale, const float* k_scale,
-                                         const float* v_scale, void* out, const dp_prefill_shape* sh, void* stream) {
+// win: the window of window_prefill_attention, null for chunked_prefill_attention
+int enqueue(const void* q, const void* k_blocks, const void* v_blocks, const int32_t* block_tables,
+            const int32_t* context_lens, const int32_t* q_start, float scale, const Window* win, const void* k_scale,
+            const void* v_scale, void* out, const dp_prefill_shape* sh, void* stream) {
   using dpool::fail;
-  if (!sh) return fail(DP_EINVAL, "chunked_prefill_attention: null shape");
-  if (sh->head_dim != kD) return fail(DP_ENOTSUP, "chunked_prefill_attention: head_dim %d (only 128)", sh->head_dim);
+  const char* const name = win ? "window_prefill_attention" : "chunked_prefill_attention";
+  if (!sh) return fail(DP_EINVAL, "%s: null shape", name);
+  if (sh->head_dim != kD) return fail(DP_ENOTSUP, "%s: head_dim %d (only 128)", name, sh->head_dim);
   if (sh->block_size != kBS)
-    return fail(DP_ENOTSUP, "chunked_prefill_attention: block_size %d (only 16)", sh->block_size);
-  if (sh->kv_dtype != DP_KV_BF16 && sh->kv_dtype != DP_KV_FP8_E4M3)
-    return fail(DP_ENOTSUP, "chunked_prefill_attention: kv_dtype %d", sh->kv_dtype);
+    return fail(DP_ENOTSUP, "%s: block_size %d (only 16)", name, sh->block_size);
+  if (sh->kv_dtype != DP_KV_BF16 && sh->kv_dtype != DP_KV_FP8_E4M3 && !(win && sh->kv_dtype == DP_KV_FP8_E4M3_BLOCK))
+    return fail(DP_ENOTSUP, "%s: kv_dtype %d", name, sh->kv_dtype);
   if (sh->out_dtype != DP_OUT_BF16 && sh->out_dtype != DP_OUT_FP32)
-    return fail(DP_ENOTSUP, "chunked_prefill_attention: out_dtype %d", sh->out_dtype);
+    return fail(DP_ENOTSUP, "%s: out_dtype %d", name, sh->out_dtype);
   if (sh->query_tile != 0 && sh->query_tile != 32)
-    return fail(DP_EINVAL, "chunked_prefill_attention: query_tile must be 0 or 32");
-  if (sh->reserved != 0) return fail(DP_EINVAL, "chunked_prefill_attention: reserved must be 0");
-  if (sh->batch < 0) return fail(DP_EINVAL, "chunked_prefill_attention: batch < 0");
-  if (sh->batch > kMaxBatch) return fail(DP_ENOTSUP, "chunked_prefill_attention: batch above 4096");
+    return fail(DP_EINVAL, "%s: query_tile must be 0 or 32", name);
+  if (sh->reserved != 0) return fail(DP_EINVAL, "%s: reserved must be 0", name);
+  if (sh->batch < 0) return fail(DP_EINVAL, "%s: batch < 0", name);
+  if (sh->batch > kMaxBatch) return fail(DP_ENOTSUP, "%s: batch above 4096", name);
   if (sh->n_kv_heads <= 0 || sh->n_q_heads <= 0 || sh->n_q_heads % sh->n_kv_heads != 0)
-    return fail(DP_EINVAL, "chunked_prefill_attention: n_q_heads must be a positive multiple of n_kv_heads");
+    return fail(DP_EINVAL, "%s: n_q_heads must be a positive multiple of n_kv_heads", name);
   if (sh->max_blocks_per_seq <= 0 || sh->max_context_len < 0 ||
       (int64_t)sh->max_blocks_per_seq * kBS < sh->max_context_len || sh->num_blocks <= 0 ||
       sh->num_blocks > INT32_MAX)
-    return fail(DP_EINVAL, "chunked_prefill_attention: need max_blocks_per_seq * 16 >= max_context_len and "
-                           "0 < num_blocks <= INT32_MAX");
-  if (sh->max_context_len > kIdCap * kBS)
-    return fail(DP_ENOTSUP, "chunked_prefill_attention: max_context_len above %d", kIdCap * kBS);
+    return fail(DP_EINVAL, "%s: need max_blocks_per_seq * 16 >= max_context_len and "
+                           "0 < num_blocks <= INT32_MAX", name);
+  if (win && (win->window < 1 || win->n_sink < 0))
+    return fail(DP_EINVAL, "%s: window %d must be at least 1, n_sink %d at least 0", name, win->window, win->n_sink);
+  if (win && sh->max_context_len > kMaxWindowContext)
+    return fail(DP_ENOTSUP, "%s: max_context_len above %d", name, kMaxWindowContext);
+  // (an item's steps hold its window, the window's growth over its 256 columns
+  // and the sinks, each rounded to steps of 64 tokens)
+  const int64_t seen = win ? std::min<int64_t>(sh->max_context_len, (int64_t)win->window + win->n_sink) : 0;
+  if (sh->max_context_len > kIdCap * kBS && !(win && seen <= kIdCap * kBS - kWindowRoom))
+    return fail(DP_ENOTSUP, "%s: max_context_len above %d", name, kIdCap * kBS);
   if (sh->total_q < 0 || sh->total_q > INT32_MAX / 2)
-    return fail(DP_EINVAL, "chunked_prefill_attention: total_q out of range");
+    return fail(DP_EINVAL, "%s: total_q out of range", name);
   if (sh->batch == 0 || sh->total_q == 0) return DP_OK;
   if (!q || !k_blocks || !v_blocks || !block_tables || !context_lens || !q_start || !out)
-    return fail(DP_EINVAL, "chunked_prefill_attention: null tensor pointer");
+    return fail(DP_EINVAL, "%s: null tensor pointer", name);
   if (((uintptr_t)q | (uintptr_t)k_blocks | (uintptr_t)v_blocks | (uintptr_t)out) & 15)
-    return fail(DP_EINVAL, "chunked_prefill_attention: q, k_blocks, v_blocks and out must be 16-byte aligned");
-  const bool fp8 = sh->kv_dtype == DP_KV_FP8_E4M3;
+    return fail(DP_EINVAL, "%s: q, k_blocks, v_blocks and out must be 16-byte aligned", name);
+  const bool fp8 = sh->kv_dtype != DP_KV_BF16;
   if (fp8 && (!k_scale || !v_scale))
-    return fail(DP_EINVAL, "chunked_prefill_attention: e4m3 cache needs k_scale and v_scale");
+    return fail(DP_EINVAL, "%s: e4m3 cache needs k_scale and v_scale", name);
   if (!fp8 && (k_scale || v_scale))
-    return fail(DP_EINVAL, "chunked_prefill_attention: k_scale/v_scale must be NULL for a bf16 cache");
+    return fail(DP_EINVAL, "%s: k_scale/v_scale must be NULL for a bf16 cache", name);
+  if (win && sh->kv_dtype == DP_KV_FP8_E4M3 && (((uintptr_t)k_scale | (uintptr_t)v_scale) & 3))
+    return fail(DP_EINVAL, "%s: k_scale and v_scale must be 4-byte aligned", name);
+  if (win && (((uintptr_t)block_tables | (uintptr_t)context_lens | (uintptr_t)q_start) & 3))
+    return fail(DP_EINVAL, "%s: block_tables, context_lens and q_start must be 4-byte aligned", name);
+  if (win && out == q) return fail(DP_EINVAL, "%s: q and out must not overlap", name);
   if (!(scale > 0.0f) || !std::isfinite(scale))
-    return fail(DP_EINVAL, "chunked_prefill_attention: scale must be finite and > 0");
+    return fail(DP_EINVAL, "%s: scale must be finite and > 0", name);
 
   const int group = sh->n_q_heads / sh->n_kv_heads;
   // The kernel counts items in 32 bits.  The bound is on tiles of 32 query
@@ -883,7 +1007,7 @@ extern "C" int chunked_prefill_attention(const void* q, const void* k_blocks, co
   // fewer items of 256 than there are compute units.
   const int64_t tiles = (sh->total_q + 31) / 32 + sh->batch;
   if (tiles * sh->n_kv_heads * (((int64_t)group + 7) / 8) > INT32_MAX / 2)
-    return fail(DP_EINVAL, "chunked_prefill_attention: too many query tiles");
+    return fail(DP_EINVAL, "%s: too many query tiles", name);
 
   PrefillArgs a;
   a.q = (const uint16_t*)q;
@@ -892,8 +1016,8 @@ extern "C" int chunked_prefill_attention(const void* q, const void* k_blocks, co
   a.block_tables = block_tables;
   a.context_lens = context_lens;
   a.q_start = q_start;
-  a.k_scale = k_scale;
-  a.v_scale = v_scale;
+  a.k_scale = (const float*)k_scale;
+  a.v_scale = (const float*)v_scale;
   a.out = out;
   a.scale_log2 = scale * kLog2e;
   a.batch = sh->batch;
@@ -905,6 +1029,11 @@ extern "C" int chunked_prefill_attention(const void* q, const void* k_blocks, co
   a.num_blocks_m1 = (int32_t)(sh->num_blocks - 1);
   a.out_fp32 = sh->out_dtype == DP_OUT_FP32;
   a.total_q = (int32_t)sh->total_q;
+  a.k_exp = (const uint8_t*)k_scale;
+  a.v_exp = (const uint8_t*)v_scale;
+  a.window = win ? std::min(win->window, std::max(a.max_ctx, 1)) : 0;
+  a.n_sink = win ? std::min(win->n_sink, a.max_ctx) : 0;
+  const Cache cache = win ? (Cache)(kWinBf16 + sh->kv_dtype) : fp8 ? kFp8 : kBf16;
   (void)hipGetLastError();
   hipStream_t st = (hipStream_t)stream;
   // The variant.  full(c): items of c columns, were the chunks one list;
@@ -940,20 +1069,43 @@ extern "C" int chunked_prefill_attention(const void* q, const void* k_blocks, co
   const int64_t per_seq = (sh->total_q * group + sh->batch - 1) / sh->batch;
   const auto full = [&](int c) { return (sh->total_q * group + c - 1) / c * sh->n_kv_heads; };
   const auto items = [&](int c) { return (per_seq + c - 1) / c * sh->batch * sh->n_kv_heads; };
-  const bool may_be_long = sh->max_context_len > 2048;
+  //  With a window, the tokens seen take the contexts' place in the rule; and
+  //  the LDS of a pair variant, its block of zeros included, does not hold the
+  //  lists of more than kMaxPairBatch sequences.
+  const bool may_be_long = win ? seen > 2048 && sh->batch <= kMaxPairBatch : sh->max_context_len > 2048;
   if (full(256) >= cus)
-    launch<8, 2, 1>(a, fp8, cus, st);
+    launch<8, 2, 1>(a, cache, cus, st);
   else if (full(128) > cus)
-    launch<4, 2, 1>(a, fp8, 2 * cus, st);
+    launch<4, 2, 1>(a, cache, 2 * cus, st);
   else if (may_be_long && full(64) <= cus && (per_seq <= 64 || items(64) <= cus))
-    launch<8, 1, 2>(a, fp8, cus, st);
+    launch<8, 1, 2>(a, cache, cus, st);
   else if (may_be_long && (per_seq <= 64 || items(128) <= cus))
-    launch<8, 2, 2>(a, fp8, cus, st);
+    launch<8, 2, 2>(a, cache, cus, st);
   else if (!may_be_long && (per_seq <= 64 || items(64) <= 2 * cus))
-    launch<4, 1, 1>(a, fp8, 2 * cus, st);
+    launch<4, 1, 1>(a, cache, 2 * cus, st);
   else
-    launch<4, 2, 1>(a, fp8, 2 * cus, st);
+    launch<4, 2, 1>(a, cache, 2 * cus, st);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(DP_EIO, "chunked_prefill_attention: kernel launch failed: %s", hipGetErrorString(e));
+  if (e != hipSuccess) return fail(DP_EIO, "%s: kernel launch failed: %s", name, hipGetErrorString(e));
   return DP_OK;
+}
+
+}  // namespace
+
+extern "C" int chunked_prefill_attention(const void* q, const void* k_blocks, const void* v_blocks,
+                                         const int32_t* block_tables, const int32_t* context_lens,
+                                         const int32_t* q_start, float scale, const float* k_scale,
+                                         const float* v_scale, void* out, const dp_prefill_shape* sh, void* stream) {
+  return enqueue(q, k_blocks, v_blocks, block_tables, context_lens, q_start, scale, nullptr, k_scale, v_scale, out, sh,
+                 stream);
+}
+
+extern "C" int window_prefill_attention(const void* q, const void* k_blocks, const void* v_blocks,
+                                        const int32_t* block_tables, const int32_t* context_lens,
+                                        const int32_t* q_start, float scale, int32_t window, int32_t n_sink,
+                                        const void* k_scale, const void* v_scale, void* out,
+                                        const dp_prefill_shape* sh, void* stream) {
+  const Window win{window, n_sink};
+  return enqueue(q, k_blocks, v_blocks, block_tables, context_lens, q_start, scale, &win, k_scale, v_scale, out, sh,
+                 stream);
 }

@@ -61,3 +61,46 @@ def test_other_entry_points_refuse_block_scales(host_lib):
     s = host_lib.decode_shape(4, 8, 2, 100, 1600, 500, block_scales=True)
     assert s.kv_dtype == host_lib.KV_FP8_E4M3_BLOCK and host_lib.workspace_size(s) == 0
     assert host_lib.lib().kv_cache_append(*[P] * 8, ctypes.byref(s), None) == ENOTSUP
+
+
+def prefill(lib, args=(), sh=(), window=64, n_sink=4, **kw):
+    s = lib.prefill_shape(**dict(dict(batch=4, n_q_heads=8, n_kv_heads=2, max_blocks_per_seq=100, max_context_len=1600,
+                                      num_blocks=500, total_q=90), **kw))
+    for k, v in dict(sh).items():
+        setattr(s, k, v)
+    fp8 = kw.get("kv_fp8") or kw.get("block_scales")
+    vals = dict(q=P, k=P, v=P, tables=P, ctx=P, q_start=P, scale=0.1, window=window, n_sink=n_sink,
+                ks=P if fp8 else None, vs=P if fp8 else None, out=2 * P)
+    vals.update(dict(args))
+    return lib.lib().window_prefill_attention(*vals.values(), ctypes.byref(s), None)
+
+
+@pytest.mark.parametrize("kw,sh,code", [
+    (dict(head_dim=64), {}, ENOTSUP), (dict(block_size=8), {}, ENOTSUP), ({}, dict(kv_dtype=3), ENOTSUP),
+    ({}, dict(out_dtype=2), ENOTSUP), ({}, dict(reserved=1), EINVAL), ({}, dict(query_tile=16), EINVAL),
+    (dict(batch=-1), {}, EINVAL), (dict(batch=4097), {}, ENOTSUP), (dict(n_q_heads=7), {}, EINVAL),
+    (dict(max_context_len=1601), {}, EINVAL), (dict(num_blocks=0), {}, EINVAL), (dict(total_q=-1), {}, EINVAL),
+    (dict(window=0), {}, EINVAL), (dict(n_sink=-1), {}, EINVAL),
+    (dict(max_blocks_per_seq=5000, max_context_len=65537, window=65000, n_sink=25), {}, ENOTSUP),
+    (dict(max_blocks_per_seq=1 << 27, max_context_len=(1 << 30) + 1), {}, ENOTSUP)])
+def test_prefill_shapes_refused(host_lib, kw, sh, code):
+    assert prefill(host_lib, sh=sh, **kw) == code
+    assert host_lib.last_error().startswith("window_prefill_attention")
+
+
+@pytest.mark.parametrize("args,kw", [
+    (dict(q=None), {}), (dict(k=None), {}), (dict(v=None), {}), (dict(tables=None), {}), (dict(ctx=None), {}),
+    (dict(q_start=None), {}), (dict(out=None), {}), (dict(ks=P, vs=P), {}), (dict(ks=None), dict(kv_fp8=True)),
+    (dict(vs=None), dict(block_scales=True)), (dict(q=P + 8), {}), (dict(v=P + 4), {}), (dict(q_start=P + 2), {}),
+    (dict(ks=P + 2), dict(kv_fp8=True)), (dict(out=P), {}), (dict(scale=0.0), {}), (dict(scale=float("inf")), {})])
+def test_prefill_pointers_refused(host_lib, args, kw):
+    assert prefill(host_lib, args, **kw) == EINVAL
+
+
+def test_chunked_prefill_refuses_block_scales(host_lib):
+    s = host_lib.prefill_shape(4, 8, 2, 100, 1600, 500, 90, block_scales=True)
+    assert host_lib.lib().chunked_prefill_attention(*[P] * 6, 0.1, P, P, 2 * P, ctypes.byref(s), None) == ENOTSUP
+
+
+def test_prefill_of_nothing_is_fine(host_lib):
+    assert prefill(host_lib, dict(q=None, out=None), total_q=0) == 0
