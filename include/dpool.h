@@ -624,6 +624,39 @@ int qk_norm_rope_append(const void* q, const void* k, const void* v, const void*
                         void* v_blocks, const float* k_scale, const float* v_scale,
                         const dp_qk_shape* shape, void* stream);
 
+/* The same into a cache with block scales (DP_KV_FP8_E4M3_BLOCK, which      */
+/* window_decode_attention and window_prefill_attention read).  k_scale and  */
+/* v_scale are [num_blocks, n_kv_heads] exponent bytes, updated in place:     */
+/* byte e stands for 2^(e - 127).  Rows that follow each other and go into   */
+/* one block form a run.  For a run, head g, and y' (K) or v (V), with s0    */
+/* the block's slot of its first row and a the largest finite magnitude      */
+/* among its rows:                                                            */
+/*     need = the smallest 2^(e - 127), 1 <= e <= 246, with a <= 448 * need  */
+/*     new  = need if s0 = 0 (the block is begun; whatever it held before    */
+/*            counts no more), else the larger of need and the block's scale */
+/*     the run's codes   = y' / new, rounded once to e4m3, ties to even      */
+/*     the slots before s0, where new is not the block's scale: their codes  */
+/*            times (old / new), rounded to e4m3: the same values, but where */
+/*            they fall below e4m3's normal range                             */
+/* Values that are not finite are stored as NaN and do not count in a.       */
+/* Slots of the block behind the run's are of no meaning.  Rows of one block */
+/* lie next to each other in the call, at most 16 of them, their slots       */
+/* rising, as kv_tables_step hands them out, and nothing else writes to the  */
+/* block meanwhile; V tiles are written whole.  Rows that break this leave   */
+/* unspecified values in their blocks, and no access leaves the buffers.     */
+/* Chains of drafts that are refused are simply written over; drafted trees, */
+/* whose accepted tokens move (kv_cache_accept), need one of the other       */
+/* cache types.                                                               */
+/* n_q_heads may be 0 (q, q_weight, q_out NULL): K and V only, which with     */
+/* rotary_dim 0 and no k_weight is a plain append.  k_scale and v_scale, and  */
+/* the two caches, are apart (DP_EINVAL where they start together).           */
+/* Everything else, errors included, is as for qk_norm_rope_append.           */
+int qk_norm_rope_append_scaled(const void* q, const void* k, const void* v, const void* q_weight,
+                               const void* k_weight, float eps, const float* cos_sin,
+                               const int32_t* positions, const int64_t* slots, void* q_out,
+                               void* k_blocks, void* v_blocks, uint8_t* k_scale, uint8_t* v_scale,
+                               const dp_qk_shape* shape, void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* Attention of drafted trees over the paged cache (device, asynchronous).  */
 /*                                                                           */

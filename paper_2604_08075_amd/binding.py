@@ -35,6 +35,7 @@ EXPORTS = (
     "paged_decode_workspace_size", "paged_decode_partition_tokens", "paged_decode_attention",
     "paged_decode_attention_noalloc", "window_decode_workspace_size", "window_decode_attention",
     "kv_cache_append", "chunked_prefill_attention", "window_prefill_attention", "kv_tables_step", "qk_norm_rope_append",
+    "qk_norm_rope_append_scaled",
     "tree_decode_workspace_size", "tree_decode_attention", "kv_cache_accept", "dp_hbm_read_probe",
 )
 
@@ -170,6 +171,7 @@ def lib() -> ctypes.CDLL:
         L.kv_tables_step.argtypes = [ctypes.c_void_p] * 15 + [ctypes.POINTER(TablesShape), ctypes.c_void_p]
         L.qk_norm_rope_append.argtypes = [ctypes.c_void_p] * 5 + [ctypes.c_float] + [ctypes.c_void_p] * 8 + [
             ctypes.POINTER(QKShape), ctypes.c_void_p]
+        L.qk_norm_rope_append_scaled.argtypes = L.qk_norm_rope_append.argtypes
         L.tree_decode_workspace_size.argtypes = [ctypes.POINTER(TreeShape)]
         L.tree_decode_workspace_size.restype = ctypes.c_size_t
         L.tree_decode_attention.argtypes = [ctypes.c_void_p] * 7 + [ctypes.c_float] + [ctypes.c_void_p] * 3 + [
@@ -460,9 +462,11 @@ def kv_tables_step(context_lens, n_owned, new_tokens, free_ids, free_state, bloc
 
 
 def qk_shape(rows, n_q_heads, n_kv_heads, num_blocks, n_positions, rotary_dim=128, interleaved=False, kv_fp8=False,
-             q_stride=None, k_stride=None, v_stride=None, head_dim=128, block_size=16) -> QKShape:
-    """Strides in elements from one row to the next; None: rows lie next to each other."""
-    return QKShape(n_q_heads, n_kv_heads, head_dim, block_size, KV_FP8_E4M3 if kv_fp8 else KV_BF16, rotary_dim,
+             q_stride=None, k_stride=None, v_stride=None, head_dim=128, block_size=16,
+             block_scales=False) -> QKShape:
+    """Strides in elements from one row to the next; None: rows lie next to each other.
+    block_scales: the shape is one of qk_norm_rope_append_scaled."""
+    return QKShape(n_q_heads, n_kv_heads, head_dim, block_size, _kv_dtype(kv_fp8, block_scales), rotary_dim,
                    int(interleaved), 0, rows, num_blocks, n_positions,
                    n_q_heads * head_dim if q_stride is None else q_stride,
                    n_kv_heads * head_dim if k_stride is None else k_stride,
@@ -485,12 +489,7 @@ def _check_rows(name, t, n, heads, head_dim, stride) -> None:
             rows *= size
 
 
-def qk_norm_rope_append(q, k, v, cos_sin, positions, slots, q_out, k_blocks, v_blocks, shape: QKShape, q_weight=None,
-                        k_weight=None, eps=1e-6, k_scale=None, v_scale=None, stream=None) -> None:
-    """Enqueue norm, rotation and cache write of the new tokens (include/dpool.h, qk_norm_rope_append).
-
-    The rows of q, k and v have to lie as far apart as the shape says, q_out
-    has to be contiguous (ValueError otherwise)."""
+def _check_qkv(q, k, v, q_out, shape) -> None:
     qs, ks, vs = shape.q_stride, shape.k_stride, shape.v_stride
     # ([rows, heads, 128] is compared first, all three at once: 0.5 us of the host)
     if (q.stride(), k.stride(), v.stride()) != ((qs, 128, 1), (ks, 128, 1), (vs, 128, 1)):
@@ -499,6 +498,15 @@ def qk_norm_rope_append(q, k, v, cos_sin, positions, slots, q_out, k_blocks, v_b
         _check_rows("v", v, shape.rows, shape.n_kv_heads, shape.head_dim, vs)
     if not q_out.is_contiguous():
         raise ValueError("q_out must be contiguous")
+
+
+def qk_norm_rope_append(q, k, v, cos_sin, positions, slots, q_out, k_blocks, v_blocks, shape: QKShape, q_weight=None,
+                        k_weight=None, eps=1e-6, k_scale=None, v_scale=None, stream=None) -> None:
+    """Enqueue norm, rotation and cache write of the new tokens (include/dpool.h, qk_norm_rope_append).
+
+    The rows of q, k and v have to lie as far apart as the shape says, q_out
+    has to be contiguous (ValueError otherwise)."""
+    _check_qkv(q, k, v, q_out, shape)
     check(lib().qk_norm_rope_append(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), q_weight.data_ptr() if q_weight is not None else None,
         k_weight.data_ptr() if k_weight is not None else None, float(eps),
@@ -506,6 +514,31 @@ def qk_norm_rope_append(q, k, v, cos_sin, positions, slots, q_out, k_blocks, v_b
         q_out.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(),
         k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None,
         ctypes.byref(shape), _stream_ptr(stream)))
+
+
+def qk_norm_rope_append_scaled(q, k, v, cos_sin, positions, slots, q_out, k_blocks, v_blocks, k_scale, v_scale,
+                               shape: QKShape, q_weight=None, k_weight=None, eps=1e-6, stream=None) -> None:
+    """Enqueue norm, rotation and the write into a cache with block scales (include/dpool.h,
+    qk_norm_rope_append_scaled); k_scale and v_scale, one byte each, are updated with it.
+
+    q and q_out may be None where the shape has no query heads.  Rows as for
+    qk_norm_rope_append; caches and scales have to be contiguous (ValueError)."""
+    if q is None:
+        _check_rows("k", k, shape.rows, shape.n_kv_heads, shape.head_dim, shape.k_stride)
+        _check_rows("v", v, shape.rows, shape.n_kv_heads, shape.head_dim, shape.v_stride)
+    else:
+        _check_qkv(q, k, v, q_out, shape)
+    if not (k_blocks.is_contiguous() and v_blocks.is_contiguous() and k_scale.is_contiguous()
+            and v_scale.is_contiguous()):
+        raise ValueError("caches and scales must be contiguous")
+    if k_scale.element_size() != 1 or v_scale.element_size() != 1:
+        raise ValueError("k_scale and v_scale hold one exponent byte for each block and head")
+    check(lib().qk_norm_rope_append_scaled(
+        q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(),
+        q_weight.data_ptr() if q_weight is not None else None, k_weight.data_ptr() if k_weight is not None else None,
+        float(eps), cos_sin.data_ptr() if cos_sin is not None else None, positions.data_ptr(), slots.data_ptr(),
+        q_out.data_ptr() if q_out is not None else None, k_blocks.data_ptr(), v_blocks.data_ptr(), k_scale.data_ptr(),
+        v_scale.data_ptr(), ctypes.byref(shape), _stream_ptr(stream)))
 
 
 def tree_shape(batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks, total_q, mask_words=1,

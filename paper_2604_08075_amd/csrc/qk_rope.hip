@@ -18,6 +18,13 @@
 // other within a block form a run; one wave takes a run's rows of one head
 // through LDS and writes each dimension's tokens together: whole 16-byte
 // pieces where the run fills them (prompts), single values otherwise.
+//
+// With block scales (qk_norm_rope_append_scaled) K and V of a run are both a
+// wave's: it has the run's values of one head in registers, takes the largest
+// magnitude over its lanes, and with it the exponent of the block's scale.
+// Earlier tokens of the block are encoded anew where the scale rises: a power of
+// two apart, so that their values stay but where they fall below e4m3's normal
+// range.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -56,6 +63,8 @@ struct RopeArgs {
   int64_t qk_groups;  // workgroups that take q and k; the others take v
   float eps;
   int32_t hq, hkv, rotary;
+  uint8_t* k_exp;  // [num_blocks, Hkv] exponent bytes (block scales)
+  uint8_t* v_exp;
 };
 
 __device__ __forceinline__ float lo_f32(int w) { return __uint_as_float((uint32_t)w << 16); }
@@ -92,11 +101,78 @@ __device__ __forceinline__ void unpack8(const i32x4& x, float* f) {
   }
 }
 
-// HG: heads per group of sixteen lanes
-template <bool FP8, bool PAIRED, int HG>
+// This lane's cosines and sines: eight pairs (halves), or four (neighbours), each used twice.
+template <bool PAIRED>
+struct Angles {
+  float cs[PAIRED ? 4 : 8], sn[PAIRED ? 4 : 8];
+};
+template <bool PAIRED>
+__device__ __forceinline__ void load_angles(const RopeArgs& a, int pos, int d0, Angles<PAIRED>& t) {
+  const int half = a.rotary >> 1;
+  const float* const row = a.cos_sin + (size_t)pos * a.rotary;
+  const int p0 = PAIRED ? d0 / 2 : d0 < half ? d0 : d0 - half;
+#pragma unroll
+  for (int i = 0; i < (PAIRED ? 4 : 8); i += 4) {
+    float4 c = {1.f, 1.f, 1.f, 1.f}, s = {0.f, 0.f, 0.f, 0.f};
+    if (d0 < a.rotary) {
+      c = *(const float4*)(row + p0 + i);
+      s = *(const float4*)(row + half + p0 + i);
+    }
+    t.cs[i] = c.x, t.cs[i + 1] = c.y, t.cs[i + 2] = c.z, t.cs[i + 3] = c.w;
+    t.sn[i] = s.x, t.sn[i + 1] = s.y, t.sn[i + 2] = s.z, t.sn[i + 3] = s.w;
+  }
+}
+
+// Norm and rotation of one head vector, dimensions d0 .. d0 + 8 of it in this lane
+// (w may be null); every lane of the group of sixteen takes part.
+template <bool PAIRED>
+__device__ __forceinline__ void turn_head(const RopeArgs& a, const i32x4& x, const uint16_t* w, const Angles<PAIRED>& t,
+                                          int d0, float (&z)[8]) {
+  const int lane = threadIdx.x & 63, l = lane & 15, half = a.rotary >> 1;
+  const bool turned = d0 < a.rotary;
+  const int mate = (lane & 48) | ((d0 < half ? l + (half >> 3) : l - (half >> 3)) & 15);
+  const float sign = d0 < half ? -1.f : 1.f;
+  float y[8];
+  unpack8(x, y);
+  float inv = 1.f;
+  if (w) {
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(y[e], y[e], ss);
+    inv = 1.0f / sqrtf(row_sum(ss) * (1.0f / kD) + a.eps);
+    float f[8];
+    unpack8(*(const i32x4*)(w + d0), f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = y[e] * inv * f[e];
+  }
+  if constexpr (PAIRED) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      z[2 * e] = turned ? y[2 * e] * t.cs[e] - y[2 * e + 1] * t.sn[e] : y[2 * e];
+      z[2 * e + 1] = turned ? y[2 * e + 1] * t.cs[e] + y[2 * e] * t.sn[e] : y[2 * e + 1];
+    }
+  } else {
+    i32x4 ox;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ox[e] = __shfl(x[e], mate);
+    float o[8];
+    unpack8(ox, o);
+    if (w) {
+      float f[8];
+      unpack8(*(const i32x4*)(w + 8 * (mate & 15)), f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = o[e] * inv * f[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = turned ? y[e] * t.cs[e] + sign * o[e] * t.sn[e] : y[e];
+  }
+}
+
+// HG: heads per group of sixteen lanes.  KEYS: k as well (else the queries only)
+template <bool FP8, bool PAIRED, int HG, bool KEYS = true>
 __device__ __forceinline__ void qk_part(const RopeArgs& a) {
   const int lane = threadIdx.x & 63, l = lane & 15;
-  const int H = a.hq + a.hkv;
+  const int H = a.hq + (KEYS ? a.hkv : 0);
   const int units = (H + HG - 1) / HG;  // per row
   const int64_t unit = ((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) * 4 + (lane >> 4);
   const int64_t r = unit / units;
@@ -107,8 +183,7 @@ __device__ __forceinline__ void qk_part(const RopeArgs& a) {
   const int64_t slot = a.slots[rc];
   if (!live || pos < 0 || pos >= a.n_positions) return;
 
-  const int d0 = 8 * l, half = a.rotary >> 1;
-  const bool turned = d0 < a.rotary;
+  const int d0 = 8 * l;
   i32x4 x[HG];
 #pragma unroll
   for (int i = 0; i < HG; ++i) {
@@ -117,64 +192,16 @@ __device__ __forceinline__ void qk_part(const RopeArgs& a) {
     else if (h < H) x[i] = *(const i32x4*)(a.k + r * a.k_stride + (h - a.hq) * kD + d0);
     else x[i] = i32x4{0, 0, 0, 0};
   }
-  // this lane's cosines and sines: eight pairs (halves), or four (neighbours), each used twice
-  float cs[PAIRED ? 4 : 8], sn[PAIRED ? 4 : 8];
-  const float* const row = a.cos_sin + (size_t)pos * a.rotary;
-  const int p0 = PAIRED ? d0 / 2 : d0 < half ? d0 : d0 - half;
-#pragma unroll
-  for (int i = 0; i < (PAIRED ? 4 : 8); i += 4) {
-    float4 c = {1.f, 1.f, 1.f, 1.f}, s = {0.f, 0.f, 0.f, 0.f};
-    if (turned) {
-      c = *(const float4*)(row + p0 + i);
-      s = *(const float4*)(row + half + p0 + i);
-    }
-    cs[i] = c.x, cs[i + 1] = c.y, cs[i + 2] = c.z, cs[i + 3] = c.w;
-    sn[i] = s.x, sn[i + 1] = s.y, sn[i + 2] = s.z, sn[i + 3] = s.w;
-  }
-  const int mate = (lane & 48) | ((d0 < half ? l + (half >> 3) : l - (half >> 3)) & 15);
-  const float sign = d0 < half ? -1.f : 1.f;
+  Angles<PAIRED> t;
+  load_angles<PAIRED>(a, pos, d0, t);
 
 #pragma unroll
   for (int i = 0; i < HG; ++i) {
     const int h = h0 + i;
     if (h >= H) break;
     const bool is_q = h < a.hq;
-    float y[8];
-    unpack8(x[i], y);
-    float inv = 1.f;
-    const uint16_t* const w = is_q ? a.q_weight : a.k_weight;
-    if (w) {
-      float ss = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(y[e], y[e], ss);
-      inv = 1.0f / sqrtf(row_sum(ss) * (1.0f / kD) + a.eps);
-      float f[8];
-      unpack8(*(const i32x4*)(w + d0), f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = y[e] * inv * f[e];
-    }
     float z[8];
-    if constexpr (PAIRED) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        z[2 * e] = turned ? y[2 * e] * cs[e] - y[2 * e + 1] * sn[e] : y[2 * e];
-        z[2 * e + 1] = turned ? y[2 * e + 1] * cs[e] + y[2 * e] * sn[e] : y[2 * e + 1];
-      }
-    } else {
-      i32x4 ox;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) ox[e] = __shfl(x[i][e], mate);
-      float o[8];
-      unpack8(ox, o);
-      if (w) {
-        float f[8];
-        unpack8(*(const i32x4*)(w + 8 * (mate & 15)), f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = o[e] * inv * f[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = turned ? y[e] * cs[e] + sign * o[e] * sn[e] : y[e];
-    }
+    turn_head<PAIRED>(a, x[i], is_q ? a.q_weight : a.k_weight, t, d0, z);
     if (is_q) {
       const i32x4 p = {pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]), pack_bf16(z[4], z[5]), pack_bf16(z[6], z[7])};
       *(i32x4*)(a.q_out + (r * a.hq + h) * kD + d0) = p;
@@ -306,6 +333,188 @@ __device__ __forceinline__ void v_part(const RopeArgs& a, uint32_t (*tile)[kD / 
   }
 }
 
+// ------------------------------------------------------------------ block scales
+
+// Largest of non-negative values over the 64 lanes, in every lane
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int m = 32; m; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
+  return x;
+}
+
+// The exponent byte of the smallest power of two over which a magnitude is at
+// most 448 = 1.75 * 2^8: its own exponent less 8, one more where its mantissa is
+// above 1.75.  At most 246, so that 448 times it is finite in bf16.
+__device__ __forceinline__ int need_byte(float a) {
+  return min(max((int)((__float_as_uint(a) + 0x1fffffu) >> 23) - 8, 1), 246);
+}
+__device__ __forceinline__ float pow2_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+
+__device__ __forceinline__ float finite_abs(float x) {
+  const float b = fabsf(x);
+  return b < INFINITY ? b : 0.f;  // (NaN too)
+}
+
+// Four values over a scale to e4m3 codes; `inv` is its inverse.  What is not
+// finite becomes NaN: no code stands for an infinity, and the largest code of a
+// block is as small as its scale.
+__device__ __forceinline__ int encode4(float a, float b, float c, float d, float inv) {
+  const auto cut = [inv](float x) {
+    const float y = fminf(fmaxf(x * inv, -kE4M3Max), kE4M3Max);
+    return fabsf(x) < INFINITY ? y : __builtin_nanf("");
+  };
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(cut(a), cut(b), 0, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(cut(c), cut(d), r, true);
+}
+
+// Four codes times a power of two, as codes (a NaN stays one).
+__device__ __forceinline__ int recode4(int w, float pow2) {
+  const auto x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, pow2, false);
+  const auto y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, pow2, true);
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], r, true);
+}
+// The factor of codes whose scale's byte rises from old to byte.
+__device__ __forceinline__ float shrink(int old, int byte) { return pow2_of(max(127 + old - byte, 0)); }
+
+// One wave: K (else V) of head g, for the runs of rows of one block that start in a window of WIN rows.
+template <bool PAIRED, int WIN>
+__device__ __forceinline__ void scaled_part(const RopeArgs& a, uint32_t (*tile)[kD / 2]) {
+  const int lane = threadIdx.x & 63, l = lane & 15, sub = lane >> 4, d0 = 8 * l;
+  const int64_t unit = ((int64_t)blockIdx.x - a.qk_groups) * kWaves + (threadIdx.x >> 6);
+  const int64_t win = unit / (2 * a.hkv);
+  const int head = (int)(unit - win * (2 * a.hkv));
+  const bool keys = head < a.hkv;
+  const int g = keys ? head : head - a.hkv;
+  const int64_t w0 = win * WIN;
+  if (w0 >= a.rows) return;
+  // lane i: row w0 - 1 + i
+  const int64_t sl = lane <= WIN + kBS ? cache_slot(a, w0 - 1 + lane) : -1;
+  const int blk = sl < 0 ? -1 : (int)(sl / kBS);
+  const int before = __shfl_up(blk, 1);
+  const bool starts = blk >= 0 && blk != before;
+  const uint64_t edges = __ballot(lane >= 1 && blk != before) | ~0ull << (WIN + kBS + 1);
+  uint64_t todo = __ballot(lane >= 1 && starts) & (((1ull << WIN) - 1) << 1);
+  while (todo) {
+    const int f = __builtin_ctzll(todo);  // the run's first row is w0 - 1 + f
+    todo &= todo - 1;
+    const uint64_t ends = edges & ~((2ull << f) - 1);
+    const int len = min(__builtin_ctzll(ends) - f, kBS);
+    const int64_t r0 = w0 - 1 + f;
+    const int off = (int)(__shfl(sl, f) % kBS);
+    const size_t at = (size_t)__shfl(blk, f) * a.hkv + g;
+    uint8_t* const exps = keys ? a.k_exp : a.v_exp;
+    const int old = off > 0 ? exps[at] : 0;
+    // rows four at a time: this lane's dimensions d0 .. d0 + 8 of rows sub, sub + 4, ..
+    if (keys) {
+      float z[4][8];
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int n = 4 * i + sub;
+        i32x4 x = {0, 0, 0, 0};
+        Angles<PAIRED> t;
+        if (n < len) {
+          x = *(const i32x4*)(a.k + (r0 + n) * a.k_stride + g * kD + d0);
+          load_angles<PAIRED>(a, a.positions[r0 + n], d0, t);
+        }
+        turn_head<PAIRED>(a, x, a.k_weight, t, d0, z[i]);
+        if (n < len)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(z[i][e]));
+      }
+      const int byte = max(need_byte(wave_max(top)), old);
+      char* const out = a.kc + at * (kBS * kD) + d0;
+      if (byte != old && off > 0) {
+        const float p = shrink(old, byte);
+        for (int n = sub; n < off; n += 4) {
+          i32x2 c = *(const i32x2*)(out + n * kD);
+          c[0] = recode4(c[0], p);
+          c[1] = recode4(c[1], p);
+          *(i32x2*)(out + n * kD) = c;
+        }
+      }
+      const float inv = pow2_of(254 - byte);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int n = 4 * i + sub;
+        const int64_t slot = __shfl(sl, f + n);
+        if (n < len) {
+          const i32x2 c = {encode4(z[i][0], z[i][1], z[i][2], z[i][3], inv),
+                           encode4(z[i][4], z[i][5], z[i][6], z[i][7], inv)};
+          *(i32x2*)(out + (int)(slot % kBS) * kD) = c;
+        }
+      }
+      if (lane == 0) exps[at] = (uint8_t)byte;
+    } else {
+      float top = 0.f;
+      for (int n = sub; n < len; n += 4) {
+        const i32x4 x = *(const i32x4*)(a.v + (r0 + n) * a.v_stride + g * kD + d0);
+        *(i32x4*)&tile[n][4 * l] = x;
+        float y[8];
+        unpack8(x, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(y[e]));
+      }
+      const int byte = max(need_byte(wave_max(top)), old);
+      const float inv = pow2_of(254 - byte);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      // This lane's dimensions 2 lane and 2 lane + 1: sixteen tokens each, written
+      // whole.  Slots that are not the run's keep their codes, those of earlier
+      // tokens under the block's scale.
+      i32x4* const out = (i32x4*)(a.vc + at * (kBS * kD) + 2 * lane * kBS);
+      i32x4 c0 = {0, 0, 0, 0}, c1 = c0;
+      if (len < kBS) {
+        c0 = out[0];
+        c1 = out[1];
+        if (byte != old && off > 0) {
+          const float p = shrink(old, byte);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = min(max(off - 4 * i, 0), 4);  // earlier tokens in this word
+            const int m = k == 4 ? -1 : (1 << (8 * k)) - 1;
+            c0[i] = (recode4(c0[i], p) & m) | (c0[i] & ~m);
+            c1[i] = (recode4(c1[i], p) & m) | (c1[i] & ~m);
+          }
+        }
+      }
+      for (int n = 0; n < len; ++n) {
+        const int slot = (int)(__shfl(sl, f + n) % kBS), sh = 8 * (slot & 3);
+        const int w = tile[n][lane];
+        const int c = encode4(lo_f32(w), hi_f32(w), 0.f, 0.f, inv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (i == slot >> 2) {
+            c0[i] = (c0[i] & ~(0xff << sh)) | ((c & 0xff) << sh);
+            c1[i] = (c1[i] & ~(0xff << sh)) | (((c >> 8) & 0xff) << sh);
+          }
+        }
+      }
+      out[0] = c0;
+      out[1] = c1;
+      if (lane == 0) exps[at] = (uint8_t)byte;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the tile is read before the next run's rows
+    }
+  }
+}
+
+template <bool PAIRED, int HG, int WIN>
+__global__ __launch_bounds__(kWaves * 64) void qk_rope_scaled_kernel(RopeArgs a) {
+  __shared__ uint32_t tile[kWaves][kBS][kD / 2];
+  if ((int64_t)blockIdx.x < a.qk_groups) qk_part<true, PAIRED, HG, false>(a);
+  else scaled_part<PAIRED, WIN>(a, tile[threadIdx.x >> 6]);
+}
+
+template <int HG, int WIN>
+void launch_scaled(RopeArgs& a, bool paired, hipStream_t st) {
+  const int64_t units = a.rows * ((a.hq + HG - 1) / HG);
+  a.qk_groups = (units + 4 * kWaves - 1) / (4 * kWaves);
+  const int64_t runs = (a.rows + WIN - 1) / WIN * (2 * a.hkv);
+  const dim3 grid((unsigned)(a.qk_groups + (runs + kWaves - 1) / kWaves)), block(kWaves * 64);
+  if (paired) hipLaunchKernelGGL((qk_rope_scaled_kernel<true, HG, WIN>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((qk_rope_scaled_kernel<false, HG, WIN>), grid, block, 0, st, a);
+}
+
 template <bool FP8, bool PAIRED, int HG, int WIN>
 __global__ __launch_bounds__(kWaves * 64) void qk_rope_kernel(RopeArgs a) {
   __shared__ uint32_t tile[kWaves][kBS][kD / 2];
@@ -329,50 +538,58 @@ void launch(RopeArgs& a, bool fp8, bool paired, hipStream_t st) {
 
 using namespace dpool_rope;
 
-extern "C" int qk_norm_rope_append(const void* q, const void* k, const void* v, const void* q_weight,
-                                   const void* k_weight, float eps, const float* cos_sin, const int32_t* positions,
-                                   const int64_t* slots, void* q_out, void* k_blocks, void* v_blocks,
-                                   const float* k_scale, const float* v_scale, const dp_qk_shape* sh, void* stream) {
+namespace {
+
+// block: the scales of qk_norm_rope_append_scaled (k_exp, v_exp), else those of qk_norm_rope_append
+int enqueue(const void* q, const void* k, const void* v, const void* q_weight, const void* k_weight, float eps,
+            const float* cos_sin, const int32_t* positions, const int64_t* slots, void* q_out, void* k_blocks,
+            void* v_blocks, const float* k_scale, const float* v_scale, bool block, uint8_t* k_exp, uint8_t* v_exp,
+            const dp_qk_shape* sh, void* stream) {
   using dpool::fail;
-  if (!sh) return fail(DP_EINVAL, "qk_norm_rope_append: null shape");
-  if (sh->head_dim != kD) return fail(DP_ENOTSUP, "qk_norm_rope_append: head_dim %d (only 128)", sh->head_dim);
-  if (sh->block_size != kBS) return fail(DP_ENOTSUP, "qk_norm_rope_append: block_size %d (only 16)", sh->block_size);
-  if (sh->kv_dtype != DP_KV_BF16 && sh->kv_dtype != DP_KV_FP8_E4M3)
-    return fail(DP_ENOTSUP, "qk_norm_rope_append: kv_dtype %d", sh->kv_dtype);
+  const char* const name = block ? "qk_norm_rope_append_scaled" : "qk_norm_rope_append";
+  if (!sh) return fail(DP_EINVAL, "%s: null shape", name);
+  if (sh->head_dim != kD) return fail(DP_ENOTSUP, "%s: head_dim %d (only 128)", name, sh->head_dim);
+  if (sh->block_size != kBS) return fail(DP_ENOTSUP, "%s: block_size %d (only 16)", name, sh->block_size);
+  if (block ? sh->kv_dtype != DP_KV_FP8_E4M3_BLOCK
+            : sh->kv_dtype != DP_KV_BF16 && sh->kv_dtype != DP_KV_FP8_E4M3)
+    return fail(DP_ENOTSUP, "%s: kv_dtype %d", name, sh->kv_dtype);
   if (sh->reserved != 0 || (sh->interleaved != 0 && sh->interleaved != 1))
-    return fail(DP_EINVAL, "qk_norm_rope_append: reserved must be 0 and interleaved 0 or 1");
+    return fail(DP_EINVAL, "%s: reserved must be 0 and interleaved 0 or 1", name);
   if (sh->rotary_dim < 0 || sh->rotary_dim > kD || sh->rotary_dim % 16 != 0)
-    return fail(DP_ENOTSUP, "qk_norm_rope_append: rotary_dim %d (a multiple of 16 up to 128)", sh->rotary_dim);
-  if (sh->n_q_heads <= 0 || sh->n_kv_heads <= 0 || sh->n_q_heads > 65536 || sh->n_kv_heads > 65536)
-    return fail(DP_EINVAL, "qk_norm_rope_append: head counts out of range");
+    return fail(DP_ENOTSUP, "%s: rotary_dim %d (a multiple of 16 up to 128)", name, sh->rotary_dim);
+  if (sh->n_q_heads < (block ? 0 : 1) || sh->n_kv_heads <= 0 || sh->n_q_heads > 65536 || sh->n_kv_heads > 65536)
+    return fail(DP_EINVAL, "%s: head counts out of range", name);
   if (sh->rows < 0 || sh->num_blocks <= 0 || sh->num_blocks > INT32_MAX || sh->n_positions <= 0 ||
       sh->n_positions > INT32_MAX)
-    return fail(DP_EINVAL, "qk_norm_rope_append: rows, num_blocks or n_positions out of range");
+    return fail(DP_EINVAL, "%s: rows, num_blocks or n_positions out of range", name);
   if (sh->rows > INT32_MAX / ((int64_t)sh->n_q_heads + 2 * (int64_t)sh->n_kv_heads))
-    return fail(DP_EINVAL, "qk_norm_rope_append: too many rows");
+    return fail(DP_EINVAL, "%s: too many rows", name);
   // (a row's heads lie next to each other, so rows closer than that would overlap)
   if (sh->q_stride < (int64_t)sh->n_q_heads * kD || sh->k_stride < (int64_t)sh->n_kv_heads * kD ||
       sh->v_stride < (int64_t)sh->n_kv_heads * kD || (sh->q_stride | sh->k_stride | sh->v_stride) % 8 != 0 ||
       std::max({sh->q_stride, sh->k_stride, sh->v_stride}) > INT64_MAX / 4 / std::max<int64_t>(sh->rows, 1))
-    return fail(DP_EINVAL, "qk_norm_rope_append: strides must be multiples of 8 that hold a row's heads");
+    return fail(DP_EINVAL, "%s: strides must be multiples of 8 that hold a row's heads", name);
   if (sh->rows == 0) return DP_OK;
-  if (!q || !k || !v || !positions || !slots || !q_out || !k_blocks || !v_blocks || (sh->rotary_dim && !cos_sin))
-    return fail(DP_EINVAL, "qk_norm_rope_append: null tensor pointer");
+  if ((sh->n_q_heads && (!q || !q_out)) || !k || !v || !positions || !slots || !k_blocks || !v_blocks ||
+      (sh->rotary_dim && !cos_sin))
+    return fail(DP_EINVAL, "%s: null tensor pointer", name);
   const bool fp8 = sh->kv_dtype == DP_KV_FP8_E4M3;
+  if (block && (!k_exp || !v_exp || k_exp == v_exp || k_blocks == v_blocks))
+    return fail(DP_EINVAL, "%s: k_scale, v_scale and the two caches must be there, and apart", name);
   if (fp8 && (!k_scale || !v_scale))
-    return fail(DP_EINVAL, "qk_norm_rope_append: e4m3 cache needs k_scale and v_scale");
+    return fail(DP_EINVAL, "%s: e4m3 cache needs k_scale and v_scale", name);
   if (!fp8 && (k_scale || v_scale))
-    return fail(DP_EINVAL, "qk_norm_rope_append: k_scale/v_scale must be NULL for a bf16 cache");
+    return fail(DP_EINVAL, "%s: k_scale/v_scale must be NULL for a bf16 cache", name);
   if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_weight | (uintptr_t)k_weight | (uintptr_t)cos_sin |
        (uintptr_t)q_out | (uintptr_t)k_blocks | (uintptr_t)v_blocks) & 15)
-    return fail(DP_EINVAL, "qk_norm_rope_append: q, k, v, weights, cos_sin, q_out and caches must be 16-byte aligned");
+    return fail(DP_EINVAL, "%s: q, k, v, weights, cos_sin, q_out and caches must be 16-byte aligned", name);
   if (((uintptr_t)positions | (uintptr_t)k_scale | (uintptr_t)v_scale) & 3 || (uintptr_t)slots & 7)
-    return fail(DP_EINVAL, "qk_norm_rope_append: positions, slots and scales must be aligned to their elements");
-  if (q_out == q && sh->q_stride != (int64_t)sh->n_q_heads * kD)
-    return fail(DP_EINVAL, "qk_norm_rope_append: q_out may be q only where q_stride is n_q_heads * 128");
-  if (q_out == k || q_out == v) return fail(DP_EINVAL, "qk_norm_rope_append: q_out must not be k or v");
+    return fail(DP_EINVAL, "%s: positions, slots and scales must be aligned to their elements", name);
+  if (q_out && q_out == q && sh->q_stride != (int64_t)sh->n_q_heads * kD)
+    return fail(DP_EINVAL, "%s: q_out may be q only where q_stride is n_q_heads * 128", name);
+  if (q_out && (q_out == k || q_out == v)) return fail(DP_EINVAL, "%s: q_out must not be k or v", name);
   if ((q_weight || k_weight) && !(eps >= 0.0f && std::isfinite(eps)))
-    return fail(DP_EINVAL, "qk_norm_rope_append: eps must be finite and >= 0");
+    return fail(DP_EINVAL, "%s: eps must be finite and >= 0", name);
 
   RopeArgs a;
   a.q = (const uint16_t*)q;
@@ -398,6 +615,8 @@ extern "C" int qk_norm_rope_append(const void* q, const void* k, const void* v, 
   a.hq = sh->n_q_heads;
   a.hkv = sh->n_kv_heads;
   a.rotary = sh->rotary_dim;
+  a.k_exp = k_exp;
+  a.v_exp = v_exp;
   (void)hipGetLastError();
   // Heads per group of lanes, and rows whose runs one wave looks for.  Few rows
   // want many waves; many rows share cosines, and prompts' runs of sixteen want
@@ -409,10 +628,34 @@ extern "C" int qk_norm_rope_append(const void* q, const void* k, const void* v, 
   // prompts gain.  Other head counts were not measured beside the rule.
   const bool paired = sh->interleaved == 1;
   hipStream_t st = (hipStream_t)stream;
-  if (sh->rows <= 256) launch<1, 1>(a, fp8, paired, st);
+  if (block) {
+    if (sh->rows <= 256) launch_scaled<1, 1>(a, paired, st);
+    else if (sh->rows < 4096) launch_scaled<2, 4>(a, paired, st);
+    else launch_scaled<2, 16>(a, paired, st);
+  } else if (sh->rows <= 256) launch<1, 1>(a, fp8, paired, st);
   else if (sh->rows < 4096) launch<2, 4>(a, fp8, paired, st);
   else launch<2, 16>(a, fp8, paired, st);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(DP_EIO, "qk_norm_rope_append: kernel launch failed: %s", hipGetErrorString(e));
+  if (e != hipSuccess) return fail(DP_EIO, "%s: kernel launch failed: %s", name, hipGetErrorString(e));
   return DP_OK;
+}
+
+}  // namespace
+
+extern "C" int qk_norm_rope_append(const void* q, const void* k, const void* v, const void* q_weight,
+                                   const void* k_weight, float eps, const float* cos_sin, const int32_t* positions,
+                                   const int64_t* slots, void* q_out, void* k_blocks, void* v_blocks,
+                                   const float* k_scale, const float* v_scale, const dp_qk_shape* shape,
+                                   void* stream) {
+  return enqueue(q, k, v, q_weight, k_weight, eps, cos_sin, positions, slots, q_out, k_blocks, v_blocks, k_scale,
+                 v_scale, false, nullptr, nullptr, shape, stream);
+}
+
+extern "C" int qk_norm_rope_append_scaled(const void* q, const void* k, const void* v, const void* q_weight,
+                                          const void* k_weight, float eps, const float* cos_sin,
+                                          const int32_t* positions, const int64_t* slots, void* q_out,
+                                          void* k_blocks, void* v_blocks, uint8_t* k_scale, uint8_t* v_scale,
+                                          const dp_qk_shape* shape, void* stream) {
+  return enqueue(q, k, v, q_weight, k_weight, eps, cos_sin, positions, slots, q_out, k_blocks, v_blocks, nullptr,
+                 nullptr, true, k_scale, v_scale, shape, stream);
 }

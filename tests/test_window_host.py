@@ -104,3 +104,55 @@ def test_chunked_prefill_refuses_block_scales(host_lib):
 
 def test_prefill_of_nothing_is_fine(host_lib):
     assert prefill(host_lib, dict(q=None, out=None), total_q=0) == 0
+
+
+def append(lib, args=(), sh=(), **kw):
+    s = lib.qk_shape(**dict(dict(rows=4, n_q_heads=8, n_kv_heads=2, num_blocks=64, n_positions=100,
+                                 block_scales=True), **kw))
+    for k, v in dict(sh).items():
+        setattr(s, k, v)
+    vals = dict(q=P, k=P, v=P, qw=None, kw=None, eps=1e-6, cos=P, pos=P, slots=P, out=2 * P, kc=3 * P, vc=4 * P,
+                ks=P + 1, vs=P + 3)
+    vals.update(dict(args))
+    return lib.lib().qk_norm_rope_append_scaled(*vals.values(), ctypes.byref(s), None)
+
+
+@pytest.mark.parametrize("kw,sh,code", [
+    (dict(head_dim=64), {}, ENOTSUP), (dict(block_size=8), {}, ENOTSUP), ({}, dict(kv_dtype=0), ENOTSUP),
+    ({}, dict(kv_dtype=1), ENOTSUP), ({}, dict(kv_dtype=3), ENOTSUP), ({}, dict(reserved=1), EINVAL),
+    ({}, dict(interleaved=2), EINVAL), (dict(rotary_dim=24), {}, ENOTSUP), (dict(n_q_heads=-1), {}, EINVAL),
+    (dict(n_kv_heads=0), {}, EINVAL), (dict(rows=-1), {}, EINVAL), (dict(rows=1 << 40), {}, EINVAL),
+    (dict(num_blocks=0), {}, EINVAL), (dict(n_positions=0), {}, EINVAL), (dict(q_stride=1016), {}, EINVAL),
+    (dict(k_stride=260), {}, EINVAL), (dict(v_stride=-256), {}, EINVAL)])
+def test_append_shapes_refused(host_lib, kw, sh, code):
+    assert append(host_lib, sh=sh, **kw) == code
+    assert host_lib.last_error().startswith("qk_norm_rope_append_scaled")
+
+
+@pytest.mark.parametrize("args,kw", [
+    (dict(q=None), {}), (dict(k=None), {}), (dict(v=None), {}), (dict(cos=None), {}), (dict(pos=None), {}),
+    (dict(slots=None), {}), (dict(out=None), {}), (dict(kc=None), {}), (dict(vc=None), {}), (dict(ks=None), {}),
+    (dict(vs=None), {}), (dict(ks=P + 3), {}), (dict(vc=3 * P), {}), (dict(q=P + 2), {}), (dict(slots=P + 4), {}),
+    (dict(out=P), dict(q_stride=2048)), (dict(kc=P + 8), {}), (dict(kw=P, eps=-1.0), {})])
+def test_append_pointers_refused(host_lib, args, kw):
+    assert append(host_lib, args, **kw) == EINVAL
+
+
+def test_append_of_nothing_is_fine(host_lib):
+    assert append(host_lib, dict(q=None, k=None), rows=0) == 0
+
+
+def test_append_binding_refuses_gaps(host_lib):
+    import torch
+    q, k = torch.zeros((4, 8, 128), dtype=torch.bfloat16), torch.zeros((4, 2, 128), dtype=torch.bfloat16)
+    c, e = torch.zeros((64, 2, 16, 128), dtype=torch.uint8), torch.zeros((64, 2), dtype=torch.uint8)
+    s, i = host_lib.qk_shape(4, 8, 2, 64, 100, block_scales=True), torch.zeros(4, dtype=torch.int64)
+    call = lambda **kw: host_lib.qk_norm_rope_append_scaled(**dict(dict(  # noqa: E731
+        q=q, k=k, v=k, cos_sin=torch.zeros(100, 128), positions=i.int(), slots=i, q_out=torch.zeros_like(q), k_blocks=c,
+        v_blocks=torch.zeros_like(c), k_scale=e, v_scale=torch.zeros_like(e), shape=s), **kw))
+    for bad in (dict(q_out=torch.zeros((4, 9, 128), dtype=torch.bfloat16)[:, :8]), dict(k=torch.zeros((8, 2, 128))[::2]),
+                dict(k_blocks=torch.zeros((64, 4, 16, 128), dtype=torch.uint8)[:, ::2]),
+                dict(v_scale=torch.zeros((64, 4), dtype=torch.uint8)[:, :2]), dict(k_scale=torch.zeros(64, 2)),
+                dict(q=None, q_out=None, v=torch.zeros((8, 2, 128))[::2])):
+        with pytest.raises(ValueError):
+            call(**bad)
