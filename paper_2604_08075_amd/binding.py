@@ -531,7 +531,7 @@ def qk_norm_rope_append_scaled(q, k, v, cos_sin, positions, slots, q_out, k_bloc
     if not (k_blocks.is_contiguous() and v_blocks.is_contiguous() and k_scale.is_contiguous()
             and v_scale.is_contiguous()):
         raise ValueError("caches and scales must be contiguous")
-    if k_scale.element_size() != 1 or v_scale.element_size() != 1:
+    if k_scale.itemsize != 1 or v_scale.itemsize != 1:
         raise ValueError("k_scale and v_scale hold one exponent byte for each block and head")
     check(lib().qk_norm_rope_append_scaled(
         q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(),

@@ -170,11 +170,11 @@ __device__ __forceinline__ void turn_head(const RopeArgs& a, const i32x4& x, con
 
 // HG: heads per group of sixteen lanes.  KEYS: k as well (else the queries only)
 template <bool FP8, bool PAIRED, int HG, bool KEYS = true>
-__device__ __forceinline__ void qk_part(const RopeArgs& a) {
+__device__ __forceinline__ void qk_part(const RopeArgs& a, int64_t group0 = 0) {
   const int lane = threadIdx.x & 63, l = lane & 15;
   const int H = a.hq + (KEYS ? a.hkv : 0);
   const int units = (H + HG - 1) / HG;  // per row
-  const int64_t unit = ((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) * 4 + (lane >> 4);
+  const int64_t unit = (((int64_t)blockIdx.x - group0) * kWaves + (threadIdx.x >> 6)) * 4 + (lane >> 4);
   const int64_t r = unit / units;
   const bool live = r < a.rows;  // (exchanges below need every lane of a group, and a group is one unit's)
   const int64_t rc = live ? r : 0;
@@ -335,11 +335,17 @@ __device__ __forceinline__ void v_part(const RopeArgs& a, uint32_t (*tile)[kD / 
 
 // ------------------------------------------------------------------ block scales
 
-// Largest of non-negative values over the 64 lanes, in every lane
+// Largest value over the 64 lanes, in every lane: rotations within the rows of
+// sixteen, then exchanges between them, all in the vector ALU
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) x = fmaxf(x, __shfl_xor(x, m));
-  return x;
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x128, 0xf, 0xf, false)));
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x124, 0xf, 0xf, false)));
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x122, 0xf, 0xf, false)));
+  x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x121, 0xf, 0xf, false)));
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // The exponent byte of the smallest power of two over which a magnitude is at
@@ -378,18 +384,39 @@ __device__ __forceinline__ int recode4(int w, float pow2) {
 __device__ __forceinline__ float shrink(int old, int byte) { return pow2_of(max(127 + old - byte, 0)); }
 
 // One wave: K (else V) of head g, for the runs of rows of one block that start in a window of WIN rows.
+//
+// Sixteen lanes hold a row, so four rows of a run are taken at a time.  K of up
+// to four rows (single tokens, most drafts) stays in registers between the
+// maximum and the codes; of longer runs it is computed again from the rows, which
+// are in the caches by then: registers for sixteen rows (170 instead of 88) cost
+// the queries' waves in the same launch their occupancy (nine prompts on 64/8
+// heads, 12,677 rows, 500 MB: 175 us; 114 so).  Sharing the angles of a run's
+// rows in LDS, or four heads of a row in one thread, came to 113 to 136.
 template <bool PAIRED, int WIN>
-__device__ __forceinline__ void scaled_part(const RopeArgs& a, uint32_t (*tile)[kD / 2]) {
+__device__ __forceinline__ void scaled_part(const RopeArgs& a, int64_t unit, uint32_t (*tile)[kD / 2]) {
   const int lane = threadIdx.x & 63, l = lane & 15, sub = lane >> 4, d0 = 8 * l;
-  const int64_t unit = ((int64_t)blockIdx.x - a.qk_groups) * kWaves + (threadIdx.x >> 6);
   const int64_t win = unit / (2 * a.hkv);
   const int head = (int)(unit - win * (2 * a.hkv));
   const bool keys = head < a.hkv;
   const int g = keys ? head : head - a.hkv;
   const int64_t w0 = win * WIN;
   if (w0 >= a.rows) return;
+  const uint16_t* const src = (keys ? a.k : a.v) + g * kD + d0;
+  const int64_t stride = keys ? a.k_stride : a.v_stride;
+  uint8_t* const exps = keys ? a.k_exp : a.v_exp;
   // lane i: row w0 - 1 + i
-  const int64_t sl = lane <= WIN + kBS ? cache_slot(a, w0 - 1 + lane) : -1;
+  const int64_t row = w0 - 1 + lane;
+  int pos = -1;
+  int64_t sl = -1;
+  if (lane <= WIN + kBS && row >= 0 && row < a.rows) {
+    pos = a.positions[row];
+    sl = a.slots[row];
+  }
+  // (with a window of one row the run, if there is one, starts there: its rows
+  // are asked for together with their slots)
+  i32x4 ahead = {0, 0, 0, 0};
+  if (WIN == 1 && w0 + sub < a.rows) ahead = *(const i32x4*)(src + (w0 + sub) * stride);
+  if (pos < 0 || pos >= a.n_positions || sl < 0 || sl >= a.n_slots) sl = -1;
   const int blk = sl < 0 ? -1 : (int)(sl / kBS);
   const int before = __shfl_up(blk, 1);
   const bool starts = blk >= 0 && blk != before;
@@ -401,30 +428,34 @@ __device__ __forceinline__ void scaled_part(const RopeArgs& a, uint32_t (*tile)[
     const uint64_t ends = edges & ~((2ull << f) - 1);
     const int len = min(__builtin_ctzll(ends) - f, kBS);
     const int64_t r0 = w0 - 1 + f;
-    const int off = (int)(__shfl(sl, f) % kBS);
-    const size_t at = (size_t)__shfl(blk, f) * a.hkv + g;
-    uint8_t* const exps = keys ? a.k_exp : a.v_exp;
+    const int off = (int)(__builtin_amdgcn_readlane((int)(sl & (kBS - 1)), f));
+    const size_t at = (size_t)__builtin_amdgcn_readlane(blk, f) * a.hkv + g;
+    const int slot = (int)(sl & (kBS - 1));  // of row w0 - 1 + lane in its block
     const int old = off > 0 ? exps[at] : 0;
-    // rows four at a time: this lane's dimensions d0 .. d0 + 8 of rows sub, sub + 4, ..
+    auto load_row = [&](int n) __attribute__((always_inline)) {
+      return WIN == 1 && n < 4 ? ahead : *(const i32x4*)(src + (r0 + n) * stride);
+    };
     if (keys) {
-      float z[4][8];
-      float top = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int n = 4 * i + sub;
-        i32x4 x = {0, 0, 0, 0};
-        Angles<PAIRED> t;
-        if (n < len) {
-          x = *(const i32x4*)(a.k + (r0 + n) * a.k_stride + g * kD + d0);
-          load_angles<PAIRED>(a, a.positions[r0 + n], d0, t);
-        }
-        turn_head<PAIRED>(a, x, a.k_weight, t, d0, z[i]);
-        if (n < len)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(z[i][e]));
-      }
-      const int byte = max(need_byte(wave_max(top)), old);
       char* const out = a.kc + at * (kBS * kD) + d0;
+      float z[8];
+      auto turned = [&](int n0) __attribute__((always_inline)) {  // z of row n0 + sub
+        const int n = n0 + sub;
+        const int p = __shfl(pos, f + n);
+        i32x4 x = {0, 0, 0, 0};
+        Angles<PAIRED> t{};
+        if (n < len) {
+          x = load_row(n);
+          load_angles<PAIRED>(a, p, d0, t);
+        }
+        turn_head<PAIRED>(a, x, a.k_weight, t, d0, z);
+        return n < len;
+      };
+      float top = 0.f;
+      for (int n0 = 0; n0 < len; n0 += 4)
+        if (turned(n0))
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(z[e]));
+      const int byte = max(need_byte(wave_max(top)), old);
       if (byte != old && off > 0) {
         const float p = shrink(old, byte);
         for (int n = sub; n < off; n += 4) {
@@ -435,21 +466,27 @@ __device__ __forceinline__ void scaled_part(const RopeArgs& a, uint32_t (*tile)[
         }
       }
       const float inv = pow2_of(254 - byte);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int n = 4 * i + sub;
-        const int64_t slot = __shfl(sl, f + n);
-        if (n < len) {
-          const i32x2 c = {encode4(z[i][0], z[i][1], z[i][2], z[i][3], inv),
-                           encode4(z[i][4], z[i][5], z[i][6], z[i][7], inv)};
-          *(i32x2*)(out + (int)(slot % kBS) * kD) = c;
-        }
+      for (int n0 = 0; n0 < len; n0 += 4) {
+        const int at_slot = __shfl(slot, f + n0 + sub);
+        if (len > 4) turned(n0);
+        if (n0 + sub < len)
+          *(i32x2*)(out + at_slot * kD) =
+              i32x2{encode4(z[0], z[1], z[2], z[3], inv), encode4(z[4], z[5], z[6], z[7], inv)};
       }
       if (lane == 0) exps[at] = (uint8_t)byte;
     } else {
+      // This lane's dimensions 2 lane and 2 lane + 1: sixteen tokens each, written
+      // whole.  Slots that are not the run's keep their codes, those of earlier
+      // tokens under the block's scale.
+      i32x4* const out = (i32x4*)(a.vc + at * (kBS * kD) + 2 * lane * kBS);
+      i32x4 c0 = {0, 0, 0, 0}, c1 = c0;
+      if (len < kBS) {
+        c0 = out[0];
+        c1 = out[1];
+      }
       float top = 0.f;
       for (int n = sub; n < len; n += 4) {
-        const i32x4 x = *(const i32x4*)(a.v + (r0 + n) * a.v_stride + g * kD + d0);
+        const i32x4 x = load_row(n);
         *(i32x4*)&tile[n][4 * l] = x;
         float y[8];
         unpack8(x, y);
@@ -459,34 +496,41 @@ __device__ __forceinline__ void scaled_part(const RopeArgs& a, uint32_t (*tile)[
       const int byte = max(need_byte(wave_max(top)), old);
       const float inv = pow2_of(254 - byte);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      // This lane's dimensions 2 lane and 2 lane + 1: sixteen tokens each, written
-      // whole.  Slots that are not the run's keep their codes, those of earlier
-      // tokens under the block's scale.
-      i32x4* const out = (i32x4*)(a.vc + at * (kBS * kD) + 2 * lane * kBS);
-      i32x4 c0 = {0, 0, 0, 0}, c1 = c0;
-      if (len < kBS) {
-        c0 = out[0];
-        c1 = out[1];
-        if (byte != old && off > 0) {
-          const float p = shrink(old, byte);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int k = min(max(off - 4 * i, 0), 4);  // earlier tokens in this word
-            const int m = k == 4 ? -1 : (1 << (8 * k)) - 1;
-            c0[i] = (recode4(c0[i], p) & m) | (c0[i] & ~m);
-            c1[i] = (recode4(c1[i], p) & m) | (c1[i] & ~m);
-          }
-        }
-      }
-      for (int n = 0; n < len; ++n) {
-        const int slot = (int)(__shfl(sl, f + n) % kBS), sh = 8 * (slot & 3);
-        const int w = tile[n][lane];
-        const int c = encode4(lo_f32(w), hi_f32(w), 0.f, 0.f, inv);
+      if (byte != old && off > 0 && len < kBS) {
+        const float p = shrink(old, byte);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (i == slot >> 2) {
-            c0[i] = (c0[i] & ~(0xff << sh)) | ((c & 0xff) << sh);
-            c1[i] = (c1[i] & ~(0xff << sh)) | (((c >> 8) & 0xff) << sh);
+          const int k = min(max(off - 4 * i, 0), 4);  // earlier tokens in this word
+          const int m = k == 4 ? -1 : (1 << (8 * k)) - 1;
+          c0[i] = (recode4(c0[i], p) & m) | (c0[i] & ~m);
+          c1[i] = (recode4(c1[i], p) & m) | (c1[i] & ~m);
+        }
+      }
+      if (len == kBS && off == 0) {
+        // a whole block (its slots rise from 0 to 15)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x[4], y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int w = tile[4 * i + e][lane];
+            x[e] = lo_f32(w);
+            y[e] = hi_f32(w);
+          }
+          c0[i] = encode4(x[0], x[1], x[2], x[3], inv);
+          c1[i] = encode4(y[0], y[1], y[2], y[3], inv);
+        }
+      } else {
+        for (int n = 0; n < len; ++n) {
+          const int to = __builtin_amdgcn_readlane(slot, f + n), sh = 8 * (to & 3);
+          const int w = tile[n][lane];
+          const int c = encode4(lo_f32(w), hi_f32(w), 0.f, 0.f, inv);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (i == to >> 2) {
+              c0[i] = (c0[i] & ~(0xff << sh)) | ((c & 0xff) << sh);
+              c1[i] = (c1[i] & ~(0xff << sh)) | (((c >> 8) & 0xff) << sh);
+            }
           }
         }
       }
@@ -501,8 +545,13 @@ __device__ __forceinline__ void scaled_part(const RopeArgs& a, uint32_t (*tile)[
 template <bool PAIRED, int HG, int WIN>
 __global__ __launch_bounds__(kWaves * 64) void qk_rope_scaled_kernel(RopeArgs a) {
   __shared__ uint32_t tile[kWaves][kBS][kD / 2];
-  if ((int64_t)blockIdx.x < a.qk_groups) qk_part<true, PAIRED, HG, false>(a);
-  else scaled_part<PAIRED, WIN>(a, tile[threadIdx.x >> 6]);
+  // K and V first: theirs are chains of dependent loads, quick while the memory
+  // is idle (one such workgroup among every eight of the queries': 148 us for 114)
+  const int64_t kv = (int64_t)gridDim.x - a.qk_groups;
+  if ((int64_t)blockIdx.x < kv)
+    scaled_part<PAIRED, WIN>(a, (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6), tile[threadIdx.x >> 6]);
+  else
+    qk_part<true, PAIRED, HG, false>(a, kv);
 }
 
 template <int HG, int WIN>
@@ -629,9 +678,14 @@ int enqueue(const void* q, const void* k, const void* v, const void* q_weight, c
   const bool paired = sh->interleaved == 1;
   hipStream_t st = (hipStream_t)stream;
   if (block) {
-    if (sh->rows <= 256) launch_scaled<1, 1>(a, paired, st);
-    else if (sh->rows < 4096) launch_scaled<2, 4>(a, paired, st);
-    else launch_scaled<2, 16>(a, paired, st);
+    // The same trade-off.  64/8 heads, us with (2, 1) / (8, 4) / (8, 16): 256 single
+    // tokens 6.6 / 7.8 / 19; 512 in runs of five 8.4 / 7.9 / 12.9; 1,024 single
+    // tokens 16.6 / 15.8 / 22.5, of prompts 20.6 / 11.2 / 12.5; 8,192 single tokens
+    // 150 / 133 / 136, of prompts 154 / 81 / 58 (eight heads a group of lanes: more
+    // loads in flight for a stream whose occupancy K's registers cut; with two 98).
+    if (sh->rows < 512) launch_scaled<2, 1>(a, paired, st);
+    else if (sh->rows < 4096) launch_scaled<8, 4>(a, paired, st);
+    else launch_scaled<8, 16>(a, paired, st);
   } else if (sh->rows <= 256) launch<1, 1>(a, fp8, paired, st);
   else if (sh->rows < 4096) launch<2, 4>(a, fp8, paired, st);
   else launch<2, 16>(a, fp8, paired, st);
