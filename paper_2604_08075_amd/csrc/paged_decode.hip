@@ -1225,113 +1225,15 @@ template __global__ void paged_decode_kernel<true, true, true>(DecodeArgs);
 constexpr int kSmallWaves = 8;
 constexpr int kSmallUnits = 2 * kSmallWaves;
 
-template <bool FP8, bool WIN, bool BLK>
-__global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(DecodeArgs a) {
-  using GE = Geo<FP8>;
-  constexpr int UB = GE::UB, UT = GE::UT, TILE = GE::TILE;
-  __shared__ __attribute__((aligned(16))) char rec[kSmallWaves][kRecBytes];
-  const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int li = lane & 15, lj = lane >> 4;
-  const int Hkv = a.hkv, G = a.group;
-  const int s = blockIdx.x / Hkv, g = blockIdx.x - s * Hkv;
-  int kofs[8], vofs[8], kblk, vblk;
-  lane_offsets<FP8>(li, lj, kofs, vofs, kblk, vblk);
-  const int ctx = clamp_ctx(a.context_lens[s], a.max_ctx);
-  const int32_t* bt = a.block_tables + (size_t)s * a.max_blocks_per_seq;
-
-  // Block ids of unit u for this lane's K and V; the sequence's last block
-  // stands in for those past its end, whose entries callers need not fill and
-  // which are never read.  (Loading them ahead of the context length, unused,
-  // saves 0.1 to 0.3 us of 8.6 to 11.0.)
-  const int last = max((ctx + kBlock - 1) / kBlock - 1, 0);
-  const Span sp = live_span<FP8, WIN>(a, ctx);
-  struct Entries { int ek, ev; };
-  auto entries = [&](int u) __attribute__((always_inline)) {
-    if constexpr (WIN) {
-      const int j = real_unit<WIN>(sp, u);
-      return Entries{bt[live_block<FP8, WIN>(a, sp, j, kblk, last + 1)],
-                     bt[live_block<FP8, WIN>(a, sp, j, vblk, last + 1)]};
-    }
-    return Entries{bt[min(u * UB + kblk, last)], bt[min(u * UB + vblk, last)]};
-  };
-  auto issue = [&](UnitRegs& R, const Entries& e) __attribute__((always_inline)) {
-    const int kt = min(max(e.ek, 0), a.num_blocks_m1) * Hkv + g, vt = min(max(e.ev, 0), a.num_blocks_m1) * Hkv + g;
-    const char* kb = a.k + (size_t)kt * TILE;
-    const char* vb = a.v + (size_t)vt * TILE;
-    if constexpr (BLK) {
-      R.ke = a.k_exp[kt];
-      R.ve = a.v_exp[vt];
-    }
-#pragma unroll
-    for (int x = 0; x < 8; ++x) R.k[x] = __builtin_nontemporal_load((const i32x4*)(kb + kofs[x]));
-#pragma unroll
-    for (int x = 0; x < 8; ++x) R.v[x] = __builtin_nontemporal_load((const i32x4*)(vb + vofs[x]));
-  };
-  const int nus = sp.nus;
-  const bool two = w + kSmallWaves < nus;
-  Entries e0{}, e1{};
-  if (w < nus) {
-    e0 = entries(w);
-    e1 = two ? entries(w + kSmallWaves) : e0;
-  }
-  i32x4 qv[4];  // columns past the GQA group repeat a real head
-  {
-    const int qhead = li < G ? li : li % G;
-    const uint16_t* qrow = a.q + ((size_t)s * a.hq + (size_t)g * G + qhead) * kHeadDim;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-      qv[c] = *(const i32x4*)(qrow + (FP8 ? 64 * (c >> 1) + 16 * lj + 8 * (c & 1) : 32 * c + 8 * lj));
-  }
-  float cscale = a.qk_scale_log2, vsc = 1.0f;
-  if constexpr (FP8 && !BLK) {
-    cscale *= a.k_scale[g];
-    vsc = a.v_scale[g];
-  }
-  float m_run = kNoScore<WIN>, l_part = 0.f;
-  f32x4 acc[8];
-#pragma unroll
-  for (int nn = 0; nn < 8; ++nn) acc[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (w < nus) {
-    UnitRegs R0, R1;
-    issue(R0, e0);
-    issue(R1, e1);  // (without a second unit the first again, unused)
-    attend_unit<FP8, WIN, BLK>(R0, qv, real_unit<WIN>(sp, w) * UT, ctx, sp.lo, a.n_sink, lj, cscale, m_run, l_part,
-                               acc);
-    if (two) {
-      // The second unit on a maximum of its own, as in slices of one unit: a
-      // probability at its unit's maximum is 1 and not rounded (a running
-      // maximum over both units: error against 64 bits 1.20e-3 of the norm,
-      // 1.18e-3 this way, over four layers of up to 512 tokens).
-      float m1 = kNoScore<WIN>, l1 = 0.f;
-      f32x4 acc1[8];
-#pragma unroll
-      for (int nn = 0; nn < 8; ++nn) acc1[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
-      attend_unit<FP8, WIN, BLK>(R1, qv, real_unit<WIN>(sp, w + kSmallWaves) * UT, ctx, sp.lo, a.n_sink, lj, cscale, m1,
-                                 l1, acc1);
-      const float M = fmaxf(m_run, m1);
-      const float w0 = __builtin_amdgcn_exp2f(m_run - M), w1 = __builtin_amdgcn_exp2f(m1 - M);
-      l_part = __builtin_fmaf(l1, w1, l_part * w0);
-#pragma unroll
-      for (int nn = 0; nn < 8; ++nn)
-        acc[nn] = __builtin_elementwise_fma(acc1[nn], f32x4{w1, w1, w1, w1}, acc[nn] * w0);
-      m_run = M;
-    }
-    // this wave's sums: eight 1 KiB chunks of o, then (m, l) per lane
-    const float l_tot = xor_sum(l_part);
-    char* base = rec[w];
-#pragma unroll
-    for (int nn = 0; nn < 8; ++nn) *(f32x4*)(base + nn * 1024 + lane * 16) = acc[nn];
-    float* ml = (float*)(base + 8192 + lane * 8);
-    ml[0] = m_run;
-    ml[1] = l_tot;
-  }
-  lds_barrier();
-  // fold, one (head, 4-value chunk) pair per thread, the waves in order
+// The output rows of segment (s, g) from the sums that the first nrec waves left
+// in LDS: one (head, 4-value chunk) pair per thread, the waves in order.
+template <bool WIN>
+__device__ __forceinline__ void fold_segment(const DecodeArgs& a, const char (*rec)[kRecBytes], int nrec, float vsc, int s,
+                                             int g) {
+  const int G = a.group;
   const int p = threadIdx.x;
   if (p >= G * 32) return;
   const int hd = p >> 5, d0 = (p & 31) * 4;
-  const int nrec = min(nus, kSmallWaves);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   if (nrec > 0) {  // (rows of empty sequences are zero)
     float M = -INFINITY, L = 0.f, m[kSmallWaves];
@@ -1362,11 +1264,228 @@ __global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(De
   }
 }
 
-template __global__ void paged_decode_small_kernel<false, false, false>(DecodeArgs);
-template __global__ void paged_decode_small_kernel<true, false, false>(DecodeArgs);
-template __global__ void paged_decode_small_kernel<false, true, false>(DecodeArgs);
-template __global__ void paged_decode_small_kernel<true, true, false>(DecodeArgs);
-template __global__ void paged_decode_small_kernel<true, true, true>(DecodeArgs);
+template <bool FP8>
+__global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(DecodeArgs a) {
+  using GE = Geo<FP8>;
+  constexpr int UB = GE::UB, UT = GE::UT, TILE = GE::TILE;
+  __shared__ __attribute__((aligned(16))) char rec[kSmallWaves][kRecBytes];
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane & 15, lj = lane >> 4;
+  const int Hkv = a.hkv, G = a.group;
+  const int s = blockIdx.x / Hkv, g = blockIdx.x - s * Hkv;
+  int kofs[8], vofs[8], kblk, vblk;
+  lane_offsets<FP8>(li, lj, kofs, vofs, kblk, vblk);
+  const int ctx = clamp_ctx(a.context_lens[s], a.max_ctx);
+  const int32_t* bt = a.block_tables + (size_t)s * a.max_blocks_per_seq;
+
+  // Block ids of unit u for this lane's K and V; the sequence's last block
+  // stands in for those past its end, whose entries callers need not fill and
+  // which are never read.  (Loading them ahead of the context length, unused,
+  // saves 0.1 to 0.3 us of 8.6 to 11.0.)
+  const int last = max((ctx + kBlock - 1) / kBlock - 1, 0);
+  struct Entries { int ek, ev; };
+  auto entries = [&](int u) __attribute__((always_inline)) {
+    return Entries{bt[min(u * UB + kblk, last)], bt[min(u * UB + vblk, last)]};
+  };
+  auto issue = [&](UnitRegs& R, const Entries& e) __attribute__((always_inline)) {
+    const int kt = min(max(e.ek, 0), a.num_blocks_m1) * Hkv + g, vt = min(max(e.ev, 0), a.num_blocks_m1) * Hkv + g;
+    const char* kb = a.k + (size_t)kt * TILE;
+    const char* vb = a.v + (size_t)vt * TILE;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) R.k[x] = __builtin_nontemporal_load((const i32x4*)(kb + kofs[x]));
+#pragma unroll
+    for (int x = 0; x < 8; ++x) R.v[x] = __builtin_nontemporal_load((const i32x4*)(vb + vofs[x]));
+  };
+  const int nus = live_span<FP8, false>(a, ctx).nus;
+  const bool two = w + kSmallWaves < nus;
+  Entries e0{}, e1{};
+  if (w < nus) {
+    e0 = entries(w);
+    e1 = two ? entries(w + kSmallWaves) : e0;
+  }
+  i32x4 qv[4];  // columns past the GQA group repeat a real head
+  {
+    const int qhead = li < G ? li : li % G;
+    const uint16_t* qrow = a.q + ((size_t)s * a.hq + (size_t)g * G + qhead) * kHeadDim;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      qv[c] = *(const i32x4*)(qrow + (FP8 ? 64 * (c >> 1) + 16 * lj + 8 * (c & 1) : 32 * c + 8 * lj));
+  }
+  float cscale = a.qk_scale_log2, vsc = 1.0f;
+  if constexpr (FP8) {
+    cscale *= a.k_scale[g];
+    vsc = a.v_scale[g];
+  }
+  float m_run = -INFINITY, l_part = 0.f;
+  f32x4 acc[8];
+#pragma unroll
+  for (int nn = 0; nn < 8; ++nn) acc[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (w < nus) {
+    UnitRegs R0, R1;
+    issue(R0, e0);
+    issue(R1, e1);  // (without a second unit the first again, unused)
+    attend_unit<FP8, false, false>(R0, qv, w * UT, ctx, 0, 0, lj, cscale, m_run, l_part, acc);
+    if (two) {
+      // The second unit on a maximum of its own, as in slices of one unit: a
+      // probability at its unit's maximum is 1 and not rounded (a running
+      // maximum over both units: error against 64 bits 1.20e-3 of the norm,
+      // 1.18e-3 this way, over four layers of up to 512 tokens).
+      float m1 = -INFINITY, l1 = 0.f;
+      f32x4 acc1[8];
+#pragma unroll
+      for (int nn = 0; nn < 8; ++nn) acc1[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
+      attend_unit<FP8, false, false>(R1, qv, (w + kSmallWaves) * UT, ctx, 0, 0, lj, cscale, m1, l1, acc1);
+      const float M = fmaxf(m_run, m1);
+      const float w0 = __builtin_amdgcn_exp2f(m_run - M), w1 = __builtin_amdgcn_exp2f(m1 - M);
+      l_part = __builtin_fmaf(l1, w1, l_part * w0);
+#pragma unroll
+      for (int nn = 0; nn < 8; ++nn)
+        acc[nn] = __builtin_elementwise_fma(acc1[nn], f32x4{w1, w1, w1, w1}, acc[nn] * w0);
+      m_run = M;
+    }
+    // this wave's sums: eight 1 KiB chunks of o, then (m, l) per lane
+    const float l_tot = xor_sum(l_part);
+    char* base = rec[w];
+#pragma unroll
+    for (int nn = 0; nn < 8; ++nn) *(f32x4*)(base + nn * 1024 + lane * 16) = acc[nn];
+    float* ml = (float*)(base + 8192 + lane * 8);
+    ml[0] = m_run;
+    ml[1] = l_tot;
+  }
+  lds_barrier();
+  fold_segment<false>(a, rec, min(nus, kSmallWaves), vsc, s, g);
+}
+
+template __global__ void paged_decode_small_kernel<false>(DecodeArgs);
+template __global__ void paged_decode_small_kernel<true>(DecodeArgs);
+
+// Windows: one workgroup per segment.
+//
+// With a window every long sequence has the same, bounded number of units, so a
+// segment to a workgroup is balanced as the batch is, and what equal slices cost
+// beside the stream is saved: the search for a slice's units, and the merge of
+// pieces through device-wide memory.  Wave w takes units w, w + 8, w + 16, at most
+// three; one load per lane fetches the table entries of all of them, a shuffle
+// hands them out, and two units are in flight at a time.  More units do not pay
+// (a loop over any number of them, times as below: window 2,048, 32 sequences
+// 35.2 / 35.1, eight 19.2 / 24.0): a compute unit's waves draw about 34 GB/s
+// whatever is in flight, and slices use all 256 units.  Measured, one layer in a
+// replayed graph, us, equal slices / here, 64/8 heads, n_sink 4:
+//   bf16, window 512 (18 units)   one sequence 11.7 / 10.6, 16: 17.7 / 13.7, 32:
+//                                 23.7 / 16.8, 32 of mixed lengths 1.31 times
+//   bf16, window 690 (24 units)   one 0.87 times as quick, 8: 0.98, 12: 1.06, 32: 1.27
+//   e4m3, window 1,024 (18 units) one 1.04 times, 16: 18.9 / 14.9, 32: 24.2 / 17.2
+//   block scales, window 1,024    one 1.00 times, 16: 18.7 / 16.0, 32: 24.4 / 19.0
+// Against two whole units a wave on maxima of their own, their entries loaded for
+// K and V apart (paged_decode_small_kernel's way): bf16, window 64, one sequence
+// 6.4 / 5.5, window 256, 32 sequences 13.8 / 10.7.
+constexpr int kWholeUnits = 3 * kSmallWaves;
+
+template <bool FP8, bool BLK>
+__global__ __launch_bounds__(kSmallWaves * 64, 2) void window_decode_kernel(DecodeArgs a) {
+  using GE = Geo<FP8>;
+  constexpr int UB = GE::UB, UT = GE::UT, TILE = GE::TILE;
+  __shared__ __attribute__((aligned(16))) char rec[kSmallWaves][kRecBytes];
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane & 15, lj = lane >> 4;
+  const int Hkv = a.hkv, G = a.group;
+  const int s = blockIdx.x / Hkv, g = blockIdx.x - s * Hkv;
+  int kofs[8], vofs[8], kblk, vblk;
+  lane_offsets<FP8>(li, lj, kofs, vofs, kblk, vblk);
+  // (every fragment's offset is a constant from the first one's)
+  constexpr int KSTEP = FP8 ? 512 : 1024, KPER = FP8 ? 2 : 4, VSTEP = FP8 ? 256 : 512;
+  const int ctx = clamp_ctx(a.context_lens[s], a.max_ctx);
+  const Span sp = live_span<FP8, true>(a, ctx);
+  const int nus = sp.nus;
+  const int n = w < nus ? (nus - w - 1) / kSmallWaves + 1 : 0;  // this wave's units
+  auto unit = [&](int k) __attribute__((always_inline)) { return real_unit<true>(sp, w + kSmallWaves * k); };
+  // lane i: tile of block i % UB of the wave's unit i / UB
+  int tile = 0;
+  if (lane < n * UB) {
+    const int nb = (ctx + kBlock - 1) / kBlock;
+    const int id = a.block_tables[(size_t)s * a.max_blocks_per_seq +
+                                  live_block<FP8, true>(a, sp, unit(lane / UB), lane % UB, nb)];
+    tile = min(max(id, 0), a.num_blocks_m1) * Hkv + g;
+  }
+  i32x4 qv[4];  // columns past the GQA group repeat a real head
+  {
+    const int qhead = li < G ? li : li % G;
+    const uint16_t* qrow = a.q + ((size_t)s * a.hq + (size_t)g * G + qhead) * kHeadDim;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      qv[c] = *(const i32x4*)(qrow + (FP8 ? 64 * (c >> 1) + 16 * lj + 8 * (c & 1) : 32 * c + 8 * lj));
+  }
+  float cscale = a.qk_scale_log2, vsc = 1.0f;
+  if constexpr (FP8 && !BLK) {
+    cscale *= a.k_scale[g];
+    vsc = a.v_scale[g];
+  }
+  // The exponent byte of 1, where the compiler does not know it: told that an e4m3
+  // code is only widened, it widens whole units ahead and spills registers.
+  int byte_one = 127;
+  asm volatile("" : "+v"(byte_one));
+  auto issue = [&](UnitRegs& R, int k) __attribute__((always_inline)) {
+    const int kt = __shfl(tile, k * UB + kblk), vt = __shfl(tile, k * UB + vblk);
+    const char* kb = a.k + (size_t)kt * TILE + kofs[0];
+    const char* vb = a.v + (size_t)vt * TILE + vofs[0];
+    if constexpr (BLK) {
+      R.ke = a.k_exp[kt];
+      R.ve = a.v_exp[vt];
+    } else {
+      R.ke = R.ve = byte_one;
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) R.k[x] = __builtin_nontemporal_load((const i32x4*)(kb + x / KPER * KSTEP + x % KPER * 64));
+#pragma unroll
+    for (int x = 0; x < 8; ++x) R.v[x] = __builtin_nontemporal_load((const i32x4*)(vb + x * VSTEP));
+  };
+  float m_run = kNoScore<true>, l_part = 0.f;
+  f32x4 acc[8];
+#pragma unroll
+  for (int nn = 0; nn < 8; ++nn) acc[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto attend = [&](const UnitRegs& R, int k) __attribute__((always_inline)) {
+    attend_unit<FP8, true, FP8>(R, qv, unit(k) * UT, ctx, sp.lo, a.n_sink, lj, cscale, m_run, l_part, acc);
+  };
+  if (n > 0) {
+    // (every path issues its loads without a condition, so that a wait for one
+    // unit never covers the next; the order is held, or units are widened ahead
+    // and registers spill)
+    UnitRegs RA, RB;
+    issue(RA, 0);
+    if (n > 1) {
+      issue(RB, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      attend(RA, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (n > 2) {
+        issue(RA, 2);
+        __builtin_amdgcn_sched_barrier(0);
+        attend(RB, 1);
+        RB = RA;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      attend(RB, n - 1);
+    } else {
+      attend(RA, 0);
+    }
+    // this wave's sums: eight 1 KiB chunks of o, then (m, l) per lane
+    const float l_tot = xor_sum(l_part);
+    char* base = rec[w];
+#pragma unroll
+    for (int nn = 0; nn < 8; ++nn) *(f32x4*)(base + nn * 1024 + lane * 16) = acc[nn];
+    float* ml = (float*)(base + 8192 + lane * 8);
+    ml[0] = m_run;
+    ml[1] = l_tot;
+  }
+  lds_barrier();
+  fold_segment<true>(a, rec, min(nus, kSmallWaves), vsc, s, g);
+}
+
+template __global__ void window_decode_kernel<false, false>(DecodeArgs);
+template __global__ void window_decode_kernel<true, false>(DecodeArgs);
+template __global__ void window_decode_kernel<true, true>(DecodeArgs);
 
 // Zero n words (arrival counters).  A kernel rather than a memset, so that a
 // captured graph holds no memset node.
@@ -1415,10 +1534,10 @@ constexpr int kVariants = 5;
 const Kernel kDecode[kVariants] = {paged_decode_kernel<false, false, false>, paged_decode_kernel<true, false, false>,
                                    paged_decode_kernel<false, true, false>, paged_decode_kernel<true, true, false>,
                                    paged_decode_kernel<true, true, true>};
-const Kernel kSmall[kVariants] = {
-    paged_decode_small_kernel<false, false, false>, paged_decode_small_kernel<true, false, false>,
-    paged_decode_small_kernel<false, true, false>, paged_decode_small_kernel<true, true, false>,
-    paged_decode_small_kernel<true, true, true>};
+// One workgroup per segment, by cache type.
+const Kernel kSmall[2] = {paged_decode_small_kernel<false>, paged_decode_small_kernel<true>};
+const Kernel kWhole[3] = {window_decode_kernel<false, false>, window_decode_kernel<true, false>,
+                          window_decode_kernel<true, true>};
 
 // Workgroups of the kernel one compute unit holds at once (register-limited;
 // runtime occupancy query, cached).  Without a device: 1.
@@ -1447,8 +1566,8 @@ struct Plan {
   size_t dyn_lds;   // dynamic LDS bytes
   size_t arrivals_off, rec_ml_off, rec_o_off, tile_cache_off, ws_bytes;
   int clear_words;  // arrival counters to zero before the launch (0 on the usual path)
-  bool small;       // one workgroup per segment
-  int variant;      // index into kDecode and kSmall
+  bool whole;       // one workgroup per segment
+  int variant;      // index into kDecode
 };
 
 constexpr int kMaxWindowContext = 1 << 30;  // positions, and a little above, are 32-bit
@@ -1529,9 +1648,11 @@ int validate(const dp_decode_shape* sh, const Window* win, Plan* plan) {
   const int64_t useful = (max_units + (int64_t)kWaves * plan->min_chunk - 1) / ((int64_t)kWaves * plan->min_chunk);
   grid = std::max<int64_t>(1, std::max(need, std::min(grid, useful)));
   plan->grid = (int)grid;
-  // (why the line lies here: at paged_decode_small_kernel)
-  plan->small = P == 0 && wpc == 0 && units_per_seq <= kSmallUnits &&
-                (int64_t)sh->batch * sh->n_kv_heads <= cus;
+  // (why the lines lie here: at paged_decode_small_kernel and window_decode_kernel)
+  const int64_t segments = (int64_t)sh->batch * sh->n_kv_heads;
+  plan->whole = P == 0 && wpc == 0 && segments <= cus &&
+                (units_per_seq <= kSmallUnits ||
+                 (win && (units_per_seq <= kSmallUnits + 2 || (units_per_seq <= kWholeUnits && 8 * segments >= 3 * cus))));
   const int G = sh->n_q_heads / sh->n_kv_heads;
   const size_t waves = (size_t)grid * kWaves;
   // The arrival counters open the workspace, and every call returns the ones
@@ -1608,8 +1729,8 @@ int enqueue(const void* q, const void* k_blocks, const void* v_blocks, const int
   a.window = win ? std::min(win->window, std::max(a.max_ctx, 1)) : 0;
   a.n_sink = win ? std::min(win->n_sink, a.max_ctx) : 0;
   (void)hipGetLastError();  // clear a stale error left by earlier work
-  if (plan.small) {
-    hipLaunchKernelGGL(kSmall[plan.variant], dim3(a.batch * a.hkv), dim3(kSmallWaves * 64), 0, (hipStream_t)stream, a);
+  if (plan.whole) {
+    hipLaunchKernelGGL(win ? kWhole[shape->kv_dtype] : kSmall[shape->kv_dtype], dim3(a.batch * a.hkv), dim3(kSmallWaves * 64), 0, (hipStream_t)stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(DP_EIO, "%s: kernel launch failed: %s", name, hipGetErrorString(e));
     return DP_OK;

@@ -179,3 +179,26 @@ def test_scale_bytes_over_the_range(gpu_lib, byte):
     got = wc.decode(gpu_lib, c, out_fp32=True).double().cpu().numpy()
     assert np.isfinite(got).all()
     assert (np.abs(got - ref) <= bound + 63 * 2.0 ** -126).all()
+
+
+# one workgroup a segment: one to three units a wave, up to one segment a compute unit, at the
+# lines of the rule (18 units at any batch, 24 from 96 segments on 256 units) and past them
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("batch,hkv", [(1, 1), (12, 8), (32, 8), (33, 8), (96, 1)])
+@pytest.mark.parametrize("units", [1, 8, 9, 16, 17, 18, 19, 22])
+def test_units_a_wave(gpu_lib, fmt, batch, hkv, units):
+    note(f"window decode {fmt} batch={batch} heads={hkv} units={units}")
+    unit = 32 if fmt == "bf16" else 64
+    rng = np.random.default_rng(units)
+    window, n_sink = max(units - 1, 1) * unit - 7, 5
+    ctx = rng.integers(1, 2 * window + 300, batch)
+    ctx[0], ctx[-1] = 2 * window + 300, window
+    c = Case(rng, ctx, None, hkv, hkv, fmt, window, n_sink)
+    pick = rng.integers(0, hkv)
+    out = wc.decode(gpu_lib, c)
+    one = Case.__new__(Case)
+    one.__dict__.update(c.__dict__)
+    one.q, one.k, one.v = c.q[:, pick:pick + 1], c.k[:, pick:pick + 1], c.v[:, pick:pick + 1]
+    if fmt != "bf16":
+        one.ks, one.vs = (x[:, pick:pick + 1] if fmt == "e4m3_block" else x[pick:pick + 1] for x in (c.ks, c.vs))
+    wc.check(out[:, pick:pick + 1], *one.oracle())
