@@ -439,11 +439,17 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
 #pragma unroll
       for (int x = 0; x < S; ++x) t.x[x] = __builtin_amdgcn_readfirstlane(id.x[x]) * a.hkv + g;
     };
+    // (BLK) 0, where the compiler takes it for a lane's own: a byte that it knows
+    // to be the same in every lane it moves to a scalar register, which waits for
+    // the load as soon as it is issued (four chunks of 2,048 tokens, 64/4 heads,
+    // window 4,096: 1,119 us, 1,005 so)
+    int lane_zero = 0;
+    if constexpr (BLK) asm volatile("" : "+v"(lane_zero));
     auto load = [&](const char* base, const uint8_t* exps, int off, const Ids& t, Chunk& r)
                     __attribute__((always_inline)) {
 #pragma unroll
       for (int x = 0; x < S; ++x) {
-        if constexpr (BLK) r.e[x] = exps[t.x[x]];
+        if constexpr (BLK) r.e[x] = exps[t.x[x] + lane_zero];
         const char* p = base + (size_t)t.x[x] * TB + off;
 #pragma unroll
         for (int y = 0; y < NL; ++y) r.x[x * NL + y] = *(const Piece*)(p + 512 * EB * y);
@@ -1073,7 +1079,13 @@ int enqueue(const void* q, const void* k_blocks, const void* v_blocks, const int
   //  the LDS of a pair variant, its block of zeros included, does not hold the
   //  lists of more than kMaxPairBatch sequences.
   const bool may_be_long = win ? seen > 2048 && sh->batch <= kMaxPairBatch : sh->max_context_len > 2048;
-  if (full(256) >= cus)
+  //  - With a window of at most 768 tokens an item has few steps, and what it
+  //    costs before and after them counts: two workgroups of 128 columns on a unit
+  //    fill each other's (64/8 heads, eleven prompts of 10,394 tokens in all, then
+  //    four chunks of 2,048: window 128, 162 -> 146 and 131 -> 121 us; window 512,
+  //    213 -> 207 and 208 -> 203; window 1,024, 254 -> 250 and 320 -> 326; window
+  //    2,048, 298 -> 309 and 562 -> 585).
+  if (full(256) >= cus && !(win && win->window <= 768))
     launch<8, 2, 1>(a, cache, cus, st);
   else if (full(128) > cus)
     launch<4, 2, 1>(a, cache, 2 * cus, st);

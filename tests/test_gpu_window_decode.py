@@ -202,3 +202,11 @@ def test_units_a_wave(gpu_lib, fmt, batch, hkv, units):
     if fmt != "bf16":
         one.ks, one.vs = (x[:, pick:pick + 1] if fmt == "e4m3_block" else x[pick:pick + 1] for x in (c.ks, c.vs))
     wc.check(out[:, pick:pick + 1], *one.oracle())
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("batch", [3, 300])
+def test_nothing_cached(gpu_lib, fmt, batch):
+    note(f"window decode {fmt} empty sequences batch={batch}")
+    c = Case(np.random.default_rng(14), [0] * batch, None, 4, 1, fmt, 10, 2)
+    assert (wc.decode(gpu_lib, c) == 0).all() and (wc.decode(gpu_lib, c, max_ctx=16) == 0).all()

@@ -10,7 +10,14 @@ attend_unit, and checks against the definition that
   * a token passes the masks exactly if the query sees it, and a unit without
     a hidden token is not masked at all;
   * the host's bound on a sequence's units is never exceeded, nor met by more
-    than two.
+    than two;
+  * where a segment is one workgroup's, its eight waves take every unit once, at
+    most three each;
+  * the prefill kernel's items: their steps hold every token that one of their
+    rows sees, block ids are staged for those alone and from entries of blocks
+    that a row sees, a wave calls a tile hidden exactly if none of its columns
+    sees it, the masking branch runs wherever a token is hidden from a column,
+    and V is zeroed exactly where no row of the item sees it.
 
 A kernel change to any of these must be mirrored here.
 """
@@ -68,6 +75,89 @@ def test_units_blocks_and_masks(ut):
                 live = first(ctx) & (~first(lo) | first(n_sink)) if ragged else (1 << nz) - 1
                 want = sum(1 << e for e in range(nz) if tok0 + e < ctx and see[tok0 + e])
                 assert live & ((1 << nz) - 1) == want
+
+
+def test_whole_segments():
+    for nus in range(0, 25):
+        mine = []
+        for w in range(8):
+            n = (nus - w - 1) // 8 + 1 if w < nus else 0
+            assert n <= 3
+            mine += [w + 8 * k for k in range(n)]
+        assert sorted(mine) == list(range(nus))
+
+
+@pytest.mark.parametrize("waves,nc,s", [(8, 2, 1), (4, 2, 1), (8, 1, 2), (8, 2, 2), (4, 1, 1)])
+def test_prefill_items(waves, nc, s):
+    rng = np.random.default_rng(waves + nc + s)
+    wave_cols = 16 * nc
+    cols, kt = wave_cols * waves // s, 32
+    st = kt * s
+    trunc = lambda a, b: int(a / b)  # noqa: E731  (C++ division)
+    trials = [(1, 1, 1, 1, 0), (33, 33, 8, 32, 1), (700, 300, 1, 64, 70), (700, 300, 16, 1, 0), (130, 2, 5, 9, 64)]
+    for _ in range(60):
+        T = int(rng.integers(1, 900))
+        trials.append((T, int(rng.integers(1, T + 1)), int(rng.choice([1, 2, 5, 8, 16])), int(rng.integers(1, 500)),
+                       int(rng.choice([0, 1, 4, 20, 64, 200]))))
+    for T, n, G, window, n_sink in trials:
+        window, n_sink = min(window, T), min(n_sink, T)
+        t = np.arange(-(-T // st) * st + st)
+        ncols, nb = n * G, -(-T // 16)
+        for qt in range(-(-ncols // cols)):
+            c0 = qt * cols
+            tok_last = (min(c0 + cols, ncols) - 1) // G
+            n_kv = T - n + tok_last + 1
+            lo = max(T - n + c0 // G - window + 1, 0)
+            head = min(-(-n_sink // st), lo // st)
+            gap = lo // st - head
+            real = lambda j: j + gap if j >= head else j  # noqa: B023, E731
+            frm = lambda r: r if r <= head else max(r - gap, head)  # noqa: B023, E731
+            nt = -(-n_kv // st) - gap
+            rows = np.arange(T - n + c0 // G, T - n + tok_last + 1)[:, None]
+            see = (t <= rows) & ((t > rows - window) | (t < n_sink))
+            steps = [real(j) for j in range(nt)]
+            assert steps == [r for r in range(len(t) // st) if see[:, r * st:(r + 1) * st].any()]
+            n_ids = min(2 * s * nt, nb - 2 * s * gap)
+            assert n_ids >= 1
+            rows_all = np.arange(T - n, T)[:, None]
+            some = ((t <= rows_all) & ((t > rows_all - window) | (t < n_sink))).any(0)
+            for i in range(n_ids):
+                b = i + 2 * s * gap if i >= 2 * s * head else i
+                e = lo // 16 if b * 16 >= n_sink and b * 16 + 16 <= lo else b
+                assert b // (2 * s) == real(i // (2 * s)) and 0 <= e < nb and some[e * 16:e * 16 + 16].any()
+            for j in range(nt):   # what is zeroed in V: hidden from every row of the item, but for causality
+                x = t[real(j) * st:(real(j) + 1) * st]
+                cut = ((x >= n_sink) & (x < lo)) | (x >= T)
+                if real(j) * st < lo and real(j) * st + st > n_sink or real(j) * st + st > T:
+                    assert not see[:, x[cut]].any()
+                else:
+                    assert not cut.any()
+            for w in range(waves):
+                ks, cg = w % s, w // s
+                if c0 + cg * wave_cols >= ncols:
+                    continue
+                pmin = T - n + min(c0 + cg * wave_cols, ncols - 1) // G
+                p_end = T - n + (min(c0 + (cg + 1) * wave_cols, ncols) - 1) // G
+                nt_w = 0 if p_end < kt * ks else frm((p_end - kt * ks) // st + 1)
+                lo_first, lo_last = pmin - window + 1, p_end - window + 1
+                j_rare = frm(min(trunc(pmin + 1 - kt * ks, st), T // st))
+                j_left = frm((max(lo_last, 0) + st - 1) // st)
+                p = np.arange(pmin, p_end + 1)[:, None]
+                for j in range(nt):
+                    t0 = st * real(j) + kt * ks
+                    x = t[t0:t0 + kt]
+                    mine = (x <= p) & ((x > p - window) | (x < n_sink))
+                    past = t0 > p_end
+                    assert not mine.any() or j < nt_w
+                    if j >= nt_w:
+                        continue
+                    hidden = t0 + kt <= lo_first and t0 >= n_sink
+                    assert past or hidden == (not mine.any())
+                    if not mine.all():
+                        assert j >= j_rare or j < j_left
+                        assert t0 + kt - 1 > pmin or (t0 < lo_last and t0 + kt > n_sink)
+                    if st * real(j) < lo and st * real(j) + st > n_sink or st * real(j) + st > T:
+                        assert j >= j_rare or j < j_left       # (the wave's part of V is zeroed there)
 
 
 def test_host_bound_is_tight():
