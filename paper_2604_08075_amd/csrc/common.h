@@ -17,4 +17,11 @@ void clear_error();
 // return for the shape, with its message recorded.
 int decode_workspace_bytes(const dp_decode_shape* shape, size_t* bytes);
 
+// Enqueue window_prefill_attention of few rows over short windows as decode's
+// one workgroup per segment does (paged_decode.hip); the arguments are valid.
+// False, nothing enqueued, if the call is not such a one.
+bool window_rows(const void* q, const void* k_blocks, const void* v_blocks, const int32_t* block_tables,
+                 const int32_t* context_lens, const int32_t* q_start, float scale, int32_t window, int32_t n_sink,
+                 const void* k_scale, const void* v_scale, void* out, const dp_prefill_shape* shape, void* stream);
+
 }  // namespace dpool

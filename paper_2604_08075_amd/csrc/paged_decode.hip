@@ -124,6 +124,8 @@ struct DecodeArgs {
   const uint8_t* k_exp;         // [num_blocks, Hkv] exponent bytes (BLK)
   const uint8_t* v_exp;
   int32_t window, n_sink;       // tokens seen up to the query's own; first tokens seen (WIN; both at most max_ctx)
+  const int32_t* q_start;       // [B + 1] (rows of several tokens)
+  int32_t total_q;
 };
 
 // Unit geometry: a unit is 16 KiB of K and V of one KV head.
@@ -199,11 +201,11 @@ struct Span {
   int nus;   // units that do
 };
 template <bool FP8, bool WIN>
-__device__ __forceinline__ Span live_span(const DecodeArgs& a, int ctx) {
+__device__ __forceinline__ Span live_span(const DecodeArgs& a, int ctx, int rows = 1) {  // the last `rows` tokens are queries
   constexpr int UT = Geo<FP8>::UT;
   Span sp{0, 0, 0, (ctx + UT - 1) / UT};
   if constexpr (WIN) {
-    sp.lo = max(ctx - a.window, 0);
+    sp.lo = max(ctx - rows + 1 - a.window, 0);
     const int first = sp.lo / UT;
     sp.head = min((a.n_sink + UT - 1) / UT, first);
     sp.gap = first - sp.head;
@@ -531,15 +533,23 @@ __device__ __forceinline__ void lane_offsets(int li, int lj, int (&kofs)[8], int
 template <bool WIN>
 constexpr float kNoScore = WIN ? -3.0e38f : -INFINITY;
 
+// Columns that are rows of several tokens: this lane's column sees tokens before
+// `end` and, past the sinks, from `lo` on; every column sees what lies before
+// `first_end` and from `last_lo` on.
+struct Cols {
+  int end, lo, first_end, last_lo;
+};
+
 // One unit of a piece: scores of the unit's tokens from unit_tok0 on (those at
 // or past ctx_s masked, and those from n_sink up to lo), online softmax, output
 // products.
-template <bool FP8, bool WIN, bool BLK>
+template <bool FP8, bool WIN, bool BLK, bool ROWS = false>
 __device__ __forceinline__ void attend_unit(const UnitRegs& R, const i32x4 (&qv)[4], int unit_tok0, int ctx_s, int lo,
                                             int n_sink, int lj, float cscale, float& m_run, float& l_part,
-                                            f32x4 (&acc)[8]) {
+                                            f32x4 (&acc)[8], const Cols& cols = Cols{}) {
   constexpr int UT = Geo<FP8>::UT, NZ = Geo<FP8>::NZ;
-  const bool ragged = unit_tok0 + UT > ctx_s || (WIN && unit_tok0 < lo && unit_tok0 + UT > n_sink);
+  const bool ragged = unit_tok0 + UT > (ROWS ? cols.first_end : ctx_s) ||
+                      (WIN && unit_tok0 < (ROWS ? cols.last_lo : lo) && unit_tok0 + UT > n_sink);
   const float kp2 = BLK ? __uint_as_float((unsigned)R.ke << 23) : 1.0f;
   const float vp2 = BLK ? __uint_as_float((unsigned)R.ve << 23) : 1.0f;
   const int lane_tok0 = unit_tok0 + (FP8 ? 16 : 8) * lj;  // first unit token of this lane's scores
@@ -576,15 +586,17 @@ __device__ __forceinline__ void attend_unit(const UnitRegs& R, const i32x4 (&qv)
   }
   // live tokens among this lane's NZ tokens (all of them unless the unit is ragged)
   const int nv = ragged ? min(max(ctx_s - lane_tok0, 0), NZ) : NZ;
-  unsigned live = (1u << NZ) - 1;  // (WIN) one bit a token
+  unsigned live = (1u << NZ) - 1;  // (WIN) one bit a token: those that some column sees
   if (ragged) {
+    unsigned mine = live;  // those that this lane's column sees
     if constexpr (WIN) {
       auto first = [&](int n) { return (1u << min(max(n - lane_tok0, 0), NZ)) - 1; };  // the tokens before token n
       live = first(ctx_s) & (~first(lo) | first(n_sink));
+      mine = ROWS ? first(cols.end) & (~first(cols.lo) | first(n_sink)) : live;
     }
 #pragma unroll
     for (int e = 0; e < NZ; ++e)
-      if (WIN ? !((live >> e) & 1) : e >= nv) z[e] = -INFINITY;
+      if (WIN ? !((mine >> e) & 1) : e >= nv) z[e] = -INFINITY;
   }
 
   // online softmax (base 2) for head li over this unit's tokens
@@ -1225,14 +1237,14 @@ template __global__ void paged_decode_kernel<true, true, true>(DecodeArgs);
 constexpr int kSmallWaves = 8;
 constexpr int kSmallUnits = 2 * kSmallWaves;
 
-// The output rows of segment (s, g) from the sums that the first nrec waves left
-// in LDS: one (head, 4-value chunk) pair per thread, the waves in order.
-template <bool WIN>
-__device__ __forceinline__ void fold_segment(const DecodeArgs& a, const char (*rec)[kRecBytes], int nrec, float vsc, int s,
-                                             int g) {
-  const int G = a.group;
+// The output rows of a workgroup's columns from the sums that the first nrec
+// waves left in LDS: one (column, 4-value chunk) pair per thread, the waves in
+// order.  row(c): the (token, head) row of column c < cols.
+template <bool WIN, class Row>
+__device__ __forceinline__ void fold_segment(const DecodeArgs& a, const char (*rec)[kRecBytes], int nrec, float vsc,
+                                             int cols, Row row) {
   const int p = threadIdx.x;
-  if (p >= G * 32) return;
+  if (p >= cols * 32) return;
   const int hd = p >> 5, d0 = (p & 31) * 4;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   if (nrec > 0) {  // (rows of empty sequences are zero)
@@ -1253,7 +1265,7 @@ __device__ __forceinline__ void fold_segment(const DecodeArgs& a, const char (*r
     }
     if (!WIN || L != 0.f) o *= vsc / L;  // (scores of -infinity alone leave zeros)
   }
-  const size_t off = ((size_t)s * a.hq + (size_t)g * G + hd) * kHeadDim + d0;
+  const size_t off = row(hd) * kHeadDim + d0;
   if (a.out_fp32) {
     *(f32x4*)((float*)a.out + off) = o;
   } else {
@@ -1354,13 +1366,19 @@ __global__ __launch_bounds__(kSmallWaves * 64) void paged_decode_small_kernel(De
     ml[1] = l_tot;
   }
   lds_barrier();
-  fold_segment<false>(a, rec, min(nus, kSmallWaves), vsc, s, g);
+  fold_segment<false>(a, rec, min(nus, kSmallWaves), vsc, G,
+                      [&](int c) { return (size_t)s * a.hq + (size_t)g * G + c; });
 }
 
 template __global__ void paged_decode_small_kernel<false>(DecodeArgs);
 template __global__ void paged_decode_small_kernel<true>(DecodeArgs);
 
-// Windows: one workgroup per segment.
+// Windows: one workgroup per segment, or (ROWS) per sixteen columns of one.
+//
+// ROWS: window_prefill_attention's calls of few rows (drafts in a row, the end of
+// a prompt).  The matrix cores' sixteen columns are (token, head) pairs of one
+// sequence and KV head, each with its own end and window; more of them are other
+// workgroups', which read the same K and V through the caches.
 //
 // With a window every long sequence has the same, bounded number of units, so a
 // segment to a workgroup is balanced as the batch is, and what equal slices cost
@@ -1382,7 +1400,7 @@ template __global__ void paged_decode_small_kernel<true>(DecodeArgs);
 // 6.4 / 5.5, window 256, 32 sequences 13.8 / 10.7.
 constexpr int kWholeUnits = 3 * kSmallWaves;
 
-template <bool FP8, bool BLK>
+template <bool FP8, bool BLK, bool ROWS>
 __global__ __launch_bounds__(kSmallWaves * 64, 2) void window_decode_kernel(DecodeArgs a) {
   using GE = Geo<FP8>;
   constexpr int UB = GE::UB, UT = GE::UT, TILE = GE::TILE;
@@ -1391,13 +1409,48 @@ __global__ __launch_bounds__(kSmallWaves * 64, 2) void window_decode_kernel(Deco
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lj = lane >> 4;
   const int Hkv = a.hkv, G = a.group;
-  const int s = blockIdx.x / Hkv, g = blockIdx.x - s * Hkv;
+  int s = blockIdx.x / Hkv;
+  const int g = blockIdx.x - s * Hkv;
   int kofs[8], vofs[8], kblk, vblk;
   lane_offsets<FP8>(li, lj, kofs, vofs, kblk, vblk);
   // (every fragment's offset is a constant from the first one's)
   constexpr int KSTEP = FP8 ? 512 : 1024, KPER = FP8 ? 2 : 4, VSTEP = FP8 ? 256 : 512;
-  const int ctx = clamp_ctx(a.context_lens[s], a.max_ctx);
-  const Span sp = live_span<FP8, true>(a, ctx);
+  int ctx, rows = 1;   // the tokens before the last column's end; how many of them are queries of the workgroup
+  int cols = G;        // columns of the workgroup
+  int col0 = 0, r0 = 0;
+  if constexpr (ROWS) {
+    // Sixteen (token, head) columns of a sequence to a workgroup, found from the
+    // row offsets, one sequence a lane.
+    const int b = min(lane, a.batch - 1);
+    const int q0 = min(max(a.q_start[b], 0), a.total_q), q1 = min(max(a.q_start[b + 1], q0), a.total_q);
+    const int T = clamp_ctx(a.context_lens[b], a.max_ctx);
+    const int n = lane < a.batch ? min(q1 - q0, T) : 0;
+    const int cnt = (n * G + 15) / 16, incl = wave_incl_scan(cnt);
+    const int item = s;
+    const unsigned long long past = __ballot(incl > item);
+    if (past == 0) return;  // (the host knows a bound on the workgroups; the same for all its waves)
+    s = __ffsll(past) - 1;
+    col0 = 16 * (item - __builtin_amdgcn_readlane(incl - cnt, s));
+    const int nn = __builtin_amdgcn_readlane(n, s);
+    cols = min(nn * G - col0, 16);
+    r0 = __builtin_amdgcn_readlane(q0, s);
+    const int last = (col0 + cols - 1) / G;  // the last column's token of the sequence's rows
+    ctx = __builtin_amdgcn_readlane(T, s) - nn + last + 1;
+    rows = last - col0 / G + 1;
+  } else {
+    ctx = clamp_ctx(a.context_lens[s], a.max_ctx);
+  }
+  // the token of the workgroup's rows and the query row of a column (those past the last repeat it)
+  auto column = [&](int c, int& tok) __attribute__((always_inline)) {
+    if constexpr (!ROWS) {
+      tok = 0;
+      return (size_t)s * a.hq + (size_t)g * G + (c < G ? c : c % G);
+    }
+    const int cc = col0 + min(c, cols - 1), x = cc / G;
+    tok = x - col0 / G;
+    return (size_t)(r0 + x) * a.hq + (size_t)(g * G + (cc - x * G));
+  };
+  const Span sp = live_span<FP8, true>(a, ctx, rows);
   const int nus = sp.nus;
   const int n = w < nus ? (nus - w - 1) / kSmallWaves + 1 : 0;  // this wave's units
   auto unit = [&](int k) __attribute__((always_inline)) { return real_unit<true>(sp, w + kSmallWaves * k); };
@@ -1409,10 +1462,15 @@ __global__ __launch_bounds__(kSmallWaves * 64, 2) void window_decode_kernel(Deco
                                   live_block<FP8, true>(a, sp, unit(lane / UB), lane % UB, nb)];
     tile = min(max(id, 0), a.num_blocks_m1) * Hkv + g;
   }
-  i32x4 qv[4];  // columns past the GQA group repeat a real head
+  i32x4 qv[4];
+  Cols col{};
   {
-    const int qhead = li < G ? li : li % G;
-    const uint16_t* qrow = a.q + ((size_t)s * a.hq + (size_t)g * G + qhead) * kHeadDim;
+    int tok;
+    const uint16_t* qrow = a.q + column(li, tok) * kHeadDim;
+    col.end = ctx - rows + 1 + tok;
+    col.lo = col.end - a.window;
+    col.first_end = ctx - rows + 1;
+    col.last_lo = ctx - a.window;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       qv[c] = *(const i32x4*)(qrow + (FP8 ? 64 * (c >> 1) + 16 * lj + 8 * (c & 1) : 32 * c + 8 * lj));
@@ -1446,7 +1504,7 @@ __global__ __launch_bounds__(kSmallWaves * 64, 2) void window_decode_kernel(Deco
 #pragma unroll
   for (int nn = 0; nn < 8; ++nn) acc[nn] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto attend = [&](const UnitRegs& R, int k) __attribute__((always_inline)) {
-    attend_unit<FP8, true, FP8>(R, qv, unit(k) * UT, ctx, sp.lo, a.n_sink, lj, cscale, m_run, l_part, acc);
+    attend_unit<FP8, true, FP8, ROWS>(R, qv, unit(k) * UT, ctx, sp.lo, a.n_sink, lj, cscale, m_run, l_part, acc, col);
   };
   if (n > 0) {
     // (every path issues its loads without a condition, so that a wait for one
@@ -1480,12 +1538,18 @@ __global__ __launch_bounds__(kSmallWaves * 64, 2) void window_decode_kernel(Deco
     ml[1] = l_tot;
   }
   lds_barrier();
-  fold_segment<true>(a, rec, min(nus, kSmallWaves), vsc, s, g);
+  fold_segment<true>(a, rec, min(nus, kSmallWaves), vsc, cols, [&](int c) {
+    int tok;
+    return column(c, tok);
+  });
 }
 
-template __global__ void window_decode_kernel<false, false>(DecodeArgs);
-template __global__ void window_decode_kernel<true, false>(DecodeArgs);
-template __global__ void window_decode_kernel<true, true>(DecodeArgs);
+template __global__ void window_decode_kernel<false, false, false>(DecodeArgs);
+template __global__ void window_decode_kernel<true, false, false>(DecodeArgs);
+template __global__ void window_decode_kernel<true, true, false>(DecodeArgs);
+template __global__ void window_decode_kernel<false, false, true>(DecodeArgs);
+template __global__ void window_decode_kernel<true, false, true>(DecodeArgs);
+template __global__ void window_decode_kernel<true, true, true>(DecodeArgs);
 
 // Zero n words (arrival counters).  A kernel rather than a memset, so that a
 // captured graph holds no memset node.
@@ -1536,8 +1600,10 @@ const Kernel kDecode[kVariants] = {paged_decode_kernel<false, false, false>, pag
                                    paged_decode_kernel<true, true, true>};
 // One workgroup per segment, by cache type.
 const Kernel kSmall[2] = {paged_decode_small_kernel<false>, paged_decode_small_kernel<true>};
-const Kernel kWhole[3] = {window_decode_kernel<false, false>, window_decode_kernel<true, false>,
-                          window_decode_kernel<true, true>};
+const Kernel kWhole[3] = {window_decode_kernel<false, false, false>, window_decode_kernel<true, false, false>,
+                          window_decode_kernel<true, true, false>};
+const Kernel kRows[3] = {window_decode_kernel<false, false, true>, window_decode_kernel<true, false, true>,
+                         window_decode_kernel<true, true, true>};
 
 // Workgroups of the kernel one compute unit holds at once (register-limited;
 // runtime occupancy query, cached).  Without a device: 1.
@@ -1745,6 +1811,53 @@ int enqueue(const void* q, const void* k_blocks, const void* v_blocks, const int
 }
 
 }  // namespace
+
+bool dpool::window_rows(const void* q, const void* k_blocks, const void* v_blocks, const int32_t* block_tables,
+                        const int32_t* context_lens, const int32_t* q_start, float scale, int32_t window,
+                        int32_t n_sink, const void* k_scale, const void* v_scale, void* out,
+                        const dp_prefill_shape* sh, void* stream) {
+  if (sh->batch > 64) return false;  // (a lane looks at each sequence)
+  const bool fp8 = sh->kv_dtype != DP_KV_BF16;
+  const int unit = fp8 ? 64 : 32, G = sh->n_q_heads / sh->n_kv_heads;
+  // sixteen columns of a sequence to a workgroup; their windows reach up to 15 tokens further than one
+  const int64_t groups = (sh->total_q * G + 15 * (int64_t)sh->batch) / 16 * sh->n_kv_heads;
+  const int64_t units = std::min(((int64_t)sh->max_context_len + unit - 1) / unit,
+                                 ((int64_t)n_sink + unit - 1) / unit + ((int64_t)window + 15 + unit - 2) / unit + 1);
+  int dev = -1;
+  // In a replayed graph, us, the prefill kernel / here, contexts of 3,000, 64/8
+  // heads: bf16, window 256, four rows of each of eight sequences 12.6 / 9.7, 64
+  // rows of one 13.4 / 10.2; window 512, 15.8 / 12.4 and 16.9 / 12.8; block scales,
+  // window 1,024, 25.8 / 15.1 and 26.1 / 15.5.  With more workgroups than compute
+  // units (24 sequences of four rows) bf16, window 64, 10.6 / 11.7, window 256,
+  // 13.2 / 18.2.
+  if (groups > device_cus(&dev) || units > kWholeUnits) return false;
+  DecodeArgs a{};
+  a.q = (const uint16_t*)q;
+  a.k = (const char*)k_blocks;
+  a.v = (const char*)v_blocks;
+  a.block_tables = block_tables;
+  a.context_lens = context_lens;
+  a.k_scale = (const float*)k_scale;
+  a.v_scale = (const float*)v_scale;
+  a.out = out;
+  a.qk_scale_log2 = scale * kLog2e;
+  a.batch = sh->batch;
+  a.hq = sh->n_q_heads;
+  a.hkv = sh->n_kv_heads;
+  a.group = G;
+  a.max_blocks_per_seq = sh->max_blocks_per_seq;
+  a.max_ctx = sh->max_context_len;
+  a.num_blocks_m1 = (int32_t)(sh->num_blocks - 1);
+  a.out_fp32 = sh->out_dtype == DP_OUT_FP32;
+  a.k_exp = (const uint8_t*)k_scale;
+  a.v_exp = (const uint8_t*)v_scale;
+  a.window = std::min(window, std::max(a.max_ctx, 1));
+  a.n_sink = std::min(n_sink, a.max_ctx);
+  a.q_start = q_start;
+  a.total_q = (int32_t)sh->total_q;
+  hipLaunchKernelGGL(kRows[sh->kv_dtype], dim3((unsigned)groups), dim3(kSmallWaves * 64), 0, (hipStream_t)stream, a);
+  return true;
+}
 
 int dpool::decode_workspace_bytes(const dp_decode_shape* shape, size_t* bytes) {
   Plan plan;

@@ -25,6 +25,11 @@ BATCHES = {"ragged": ([1, 16, 33, 200, 64, 300], [1, 16, 2, 150, 64, 7]),
            "gaps": ([400, 5, 40], [65, 0, 0])}
 
 
+def crowded(ctx, rows):
+    """The same sequences among enough others without rows that a batch is not one of few rows (64 sequences)."""
+    return list(ctx) + [3] * 64, list(rows) + [0] * 64
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("window,n_sink", EDGES)
 @pytest.mark.parametrize("batch", list(BATCHES))
@@ -34,33 +39,41 @@ def test_windows(gpu_lib, fmt, window, n_sink, batch):
     c = Case(rng, *BATCHES[batch], 8, 2, fmt, window, n_sink)
     ref, bound = c.oracle()
     wc.check(wc.prefill(gpu_lib, c), ref, bound)
-    # contexts that may be long take other variants (pairs of waves)
-    c.max_blocks, c.tables = 300, np.pad(c.tables, ((0, 0), (0, 300 - c.tables.shape[1])), constant_values=-1)
+    wc.check(wc.prefill(gpu_lib, c, max_ctx=4800 if c.max_blocks >= 300 else 16 * c.max_blocks, out_fp32=True), ref,
+             bound)
+    c = Case(rng, *crowded(*BATCHES[batch]), 8, 2, fmt, window, n_sink, max_blocks=300)
+    ref, bound = c.oracle()
+    wc.check(wc.prefill(gpu_lib, c), ref, bound)
+    # contexts that may be long take other variants (pairs of waves) where the window is wide
     wc.check(wc.prefill(gpu_lib, c, max_ctx=4800, out_fp32=True), ref, bound)
 
 
-# columns of the batch against the launch rule's lines: 256 columns to eight
-# waves, 128 to four, 64 and 128 to pairs, 64 to four
+# batches on each side of the launch rule's lines: 256 columns to eight waves, 128
+# to four, 64 and 128 to pairs, 64 to four (a batch of more than 64), few rows
+VARIANTS = {
+    "256": ([1000] * 4, [512] * 4, 64, 32, 63, 800, 5), "128": ([600] * 3, [350] * 3, 64, 32, 40, 290, 0),
+    "128 short": ([600] * 3, [350] * 3, 64, 32, 40, 70, 5), "pairs 64": ([2600, 90], [100, 90], 16, 2, 200, 2100, 3),
+    "pairs 128": ([2600, 2300], [150, 150], 64, 2, 200, 2100, 0), "64": ([200] * 70, [3] * 70, 8, 4, 20, 70, 5),
+    "few": ([600, 90], [100, 90], 16, 2, 40, 290, 5), "few, many heads": ([300, 90], [9, 7], 64, 1, 40, 64, 1)}
+
+
 @pytest.mark.parametrize("fmt", FMTS)
-@pytest.mark.parametrize("ctx,rows,hq,hkv,max_blocks", [
-    ([600] * 4, [512] * 4, 64, 32, 40), ([600] * 3, [350] * 3, 64, 32, 40), ([600, 90], [100, 90], 16, 2, 200),
-    ([900, 900], [128, 128], 64, 2, 200), ([100] * 9, [40] * 9, 8, 4, 10)])
-@pytest.mark.parametrize("window,n_sink", [(70, 5), (290, 0)])
-def test_variants(gpu_lib, fmt, ctx, rows, hq, hkv, max_blocks, window, n_sink):
-    note(f"window prefill {fmt} rows={rows} heads={hq}/{hkv} window={window} sinks={n_sink}")
+@pytest.mark.parametrize("variant", list(VARIANTS))
+def test_variants(gpu_lib, fmt, variant):
+    ctx, rows, hq, hkv, max_blocks, window, n_sink = VARIANTS[variant]
+    note(f"window prefill {fmt} variant {variant}")
     rng = np.random.default_rng(hq + window)
     c = Case(rng, ctx, rows, hq, hkv, fmt, window, n_sink, max_blocks=max_blocks)
     out = wc.prefill(gpu_lib, c, max_ctx=max_blocks * 16)
-    c1 = c
     if hkv == 32:  # a head of each launch is enough for the oracle
-        got = out.view(c.total, hkv, hq // hkv, 128)[:, 5].contiguous()
-        c1 = Case.__new__(Case)
-        c1.__dict__.update(c.__dict__)
-        c1.q, c1.k, c1.v = c.q.reshape(c.total, hkv, -1, 128)[:, 5], c.k[:, 5:6], c.v[:, 5:6]
+        out = out.view(c.total, hkv, hq // hkv, 128)[:, 5].contiguous()
+        one = Case.__new__(Case)
+        one.__dict__.update(c.__dict__)
+        one.q, one.k, one.v = c.q.reshape(c.total, hkv, -1, 128)[:, 5], c.k[:, 5:6], c.v[:, 5:6]
         if fmt != "bf16":
-            c1.ks, c1.vs = (x[:, 5:6] if fmt == "e4m3_block" else x[5:6] for x in (c.ks, c.vs))
-        out = got
-    wc.check(out, *c1.oracle())
+            one.ks, one.vs = (x[:, 5:6] if fmt == "e4m3_block" else x[5:6] for x in (c.ks, c.vs))
+        c = one
+    wc.check(out, *c.oracle())
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -69,6 +82,8 @@ def test_heads(gpu_lib, fmt, hq, hkv):
     note(f"window prefill {fmt} heads {hq}/{hkv}")
     rng = np.random.default_rng(hq)
     c = Case(rng, [290, 40, 500], [290, 3, 66], hq, hkv, fmt, 120, 20)
+    wc.check(wc.prefill(gpu_lib, c), *c.oracle())
+    c = Case(rng, *crowded([290, 40, 500], [290, 3, 66]), hq, hkv, fmt, 120, 20)
     wc.check(wc.prefill(gpu_lib, c), *c.oracle())
 
 
@@ -85,10 +100,11 @@ def test_decode_is_the_case_of_one_row(gpu_lib, fmt):
 @pytest.mark.parametrize("fmt", ["bf16", "fp8_e4m3"])
 @pytest.mark.parametrize("max_blocks", [40, 300])
 def test_whole_contexts_agree_with_chunked_prefill(gpu_lib, fmt, max_blocks):
-    """A window that hides nothing: the same arithmetic as the call without one, bit for bit."""
+    """A window that hides nothing, in a batch that is not one of few rows: the same arithmetic as the call without
+    one, bit for bit."""
     note(f"window prefill {fmt} against chunked_prefill_attention")
     rng = np.random.default_rng(6)
-    c = Case(rng, [600, 33, 1], [200, 33, 1], 16, 2, fmt, 10000, 0, max_blocks=max_blocks)
+    c = Case(rng, [600, 33, 1], [200, 33, 1], 32, 8, fmt, 10000, 0, max_blocks=max_blocks)
     d = c.device()
     a = wc.prefill(gpu_lib, c, d=d, max_ctx=16 * max_blocks)
     b = torch.empty_like(a)
@@ -102,8 +118,9 @@ def test_context_past_the_staged_ids(gpu_lib, fmt):
     """A context of more than 65,536 tokens, of which the window leaves few."""
     note(f"window prefill {fmt} long context")
     rng = np.random.default_rng(7)
-    c = Case(rng, [200_003, 90], [70, 5], 2, 1, fmt, 333, 40)
-    wc.check(wc.prefill(gpu_lib, c), *c.oracle())
+    for ctx, rows in (([200_003, 90], [70, 5]), crowded([200_003, 90], [70, 5])):
+        c = Case(rng, ctx, rows, 2, 1, fmt, 333, 40)
+        wc.check(wc.prefill(gpu_lib, c), *c.oracle())
 
 
 def test_widest_window_past_the_staged_ids(gpu_lib):
@@ -132,12 +149,13 @@ def test_widest_window_past_the_staged_ids(gpu_lib):
 
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("hq,hkv", [(8, 1), (1, 1)])
-def test_a_value_that_is_not_finite_stays_near(gpu_lib, fmt, hq, hkv):
+@pytest.mark.parametrize("many", [False, True])
+def test_a_value_that_is_not_finite_stays_near(gpu_lib, fmt, hq, hkv, many):
     """NaN in the rows that see its token, in none farther than 62 positions from those."""
     note(f"window prefill {fmt} NaN value heads {hq}/{hkv}")
     rng = np.random.default_rng(9)
     T, n, window, sinks = 900, 600, 100, 8
-    c = Case(rng, [T], [n], hq, hkv, fmt, window, sinks)
+    c = Case(rng, *(crowded([T], [n]) if many else ([T], [n])), hq, hkv, fmt, window, sinks)
     see = ow.sees(T, n, window, sinks)
     for t in (3, 250, 555, 899):
         d = c.device()
@@ -151,11 +169,13 @@ def test_a_value_that_is_not_finite_stays_near(gpu_lib, fmt, hq, hkv):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp8_e4m3"])
-@pytest.mark.parametrize("max_blocks", [20, 300])
-def test_scores_of_minus_infinity_and_odd_scales(gpu_lib, fmt, max_blocks):
+@pytest.mark.parametrize("max_blocks,many", [(20, False), (20, True), (300, True)])
+@pytest.mark.parametrize("window", [70, 3000])
+def test_scores_of_minus_infinity_and_odd_scales(gpu_lib, fmt, max_blocks, many, window):
     note(f"window prefill {fmt} infinite scores, odd scales")
     rng = np.random.default_rng(10)
-    c = Case(rng, [100, 300], [20, 30], 4, 2, fmt, 70, 2, max_blocks=max_blocks)
+    c = Case(rng, *(crowded([100, 300], [20, 30]) if many else ([100, 300], [20, 30])), 4, 2, fmt, window, 2,
+             max_blocks=max_blocks)
     c.q[:, :, 0] = 0x3F80
     if fmt == "bf16":
         c.k[c.tables[0, :7], 0, :, 0] = 0xFF80
@@ -172,10 +192,11 @@ def test_scores_of_minus_infinity_and_odd_scales(gpu_lib, fmt, max_blocks):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
-def test_rows_behind_the_batch_stay(gpu_lib, fmt):
+@pytest.mark.parametrize("many", [False, True])
+def test_rows_behind_the_batch_stay(gpu_lib, fmt, many):
     note(f"window prefill {fmt} padded batch")
     rng = np.random.default_rng(11)
-    c = Case(rng, [60, 30], [20, 30], 4, 2, fmt, 25, 2)
+    c = Case(rng, *(crowded([60, 30], [20, 30]) if many else ([60, 30], [20, 30])), 4, 2, fmt, 25, 2)
     ref, bound = c.oracle()
     d = c.device()
     pad = torch.zeros((13, 4, 128), dtype=d["q"].dtype, device="cuda")
@@ -188,10 +209,11 @@ def test_rows_behind_the_batch_stay(gpu_lib, fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
-def test_captured_replayed_and_on_two_streams(gpu_lib, fmt):
+@pytest.mark.parametrize("many", [False, True])
+def test_captured_replayed_and_on_two_streams(gpu_lib, fmt, many):
     note(f"window prefill {fmt} graph and streams")
     rng = np.random.default_rng(12)
-    c = Case(rng, [500, 31, 90], [130, 20, 90], 8, 2, fmt, 64, 4)
+    c = Case(rng, *(crowded([500, 31, 90], [130, 20, 90]) if many else ([500, 31, 90], [130, 20, 90])), 8, 2, fmt, 64, 4)
     d = c.device()
     want = wc.prefill(gpu_lib, c, d=d).clone()
     outs = [torch.zeros_like(want) for _ in range(2)]
@@ -225,3 +247,44 @@ def test_largest_batches(gpu_lib, batch):
         c = Case(rng, ctx, np.ones(batch, np.int64), 2, 1, fmt, 3000, 1, max_blocks=200)
         ref, bound = c.oracle()
         wc.check(wc.prefill(gpu_lib, c, max_ctx=3200), ref, bound)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("batch", [64, 65])
+def test_few_rows_of_many_sequences(gpu_lib, fmt, batch):
+    """Row offsets of up to 64 sequences are looked at by the lanes of a wave; some have no rows, some no tokens."""
+    note(f"window prefill {fmt} {batch} sequences")
+    rng = np.random.default_rng(batch)
+    ctx = rng.integers(0, 300, batch)
+    rows = np.minimum(rng.integers(0, 4, batch), ctx)
+    rows[-1], ctx[-1] = 3, 250
+    c = Case(rng, ctx, rows, 5, 1, fmt, 90, 3)
+    wc.check(wc.prefill(gpu_lib, c), *c.oracle())
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3_block"])
+def test_broken_promises_stay_in_bounds(gpu_lib, fmt):
+    """Row offsets out of order or past total_q, more rows than tokens, contexts past the largest, ids outside the
+    pool: clamped, and rows past the clamped ones are left alone."""
+    note(f"window prefill {fmt} broken promises")
+    rng = np.random.default_rng(15)
+    for many in (False, True):
+        ctx, rows = ([40, 200, 64], [10, 20, 5])
+        if many:
+            ctx, rows = crowded(ctx, rows)
+        c = Case(rng, ctx, rows, 4, 2, fmt, 50, 3)
+        ref, bound = c.oracle()
+        d = c.device()
+        d["tables"][1] = 1 << 30                               # (sequence 1's blocks: any of the pool's)
+        d["ctx"][2] = 1 << 20                                  # longer than max_context_len: clamped
+        got = wc.prefill(gpu_lib, c, d=d).double().cpu().numpy()
+        assert (np.abs(got[:10] - ref[:10]) <= bound[:10]).all()
+        d = c.device()
+        d["ctx"][0] = 4                                        # ten rows of four tokens: six are left alone
+        d["q_start"][3:] = 1 << 20                             # ends past total_q
+        out = torch.full((c.total, 4, 128), 5.0, dtype=torch.bfloat16, device="cuda")
+        wc.prefill(gpu_lib, c, d=d, out=out)
+        assert (out[4:10] == 5.0).all() and (out[:4] != 5.0).any()
+        d["q_start"][1:] = torch.flip(d["q_start"][1:], (0,))  # out of order
+        wc.prefill(gpu_lib, c, d=d, out=out)
+        torch.cuda.synchronize()

@@ -166,3 +166,38 @@ def test_host_bound_is_tight():
         for ctx in range(window, window + 70):
             worst = max(worst, host_bound(ctx, window, 0, 32) - span(ctx, window, 0, 32)[3])
     assert worst <= 2
+
+
+def test_few_rows_workgroups():
+    """The workgroups of few rows: every (token, head) column once, none past the host's bound."""
+    rng = np.random.default_rng(3)
+    for _ in range(300):
+        batch, G, hkv = int(rng.integers(1, 65)), int(rng.choice([1, 2, 5, 8, 16, 40])), 3
+        T = rng.integers(0, 50, batch)
+        asked = rng.integers(0, 6, batch)
+        total_q = int(asked.sum())
+        n = np.minimum(asked, T)                       # (rows past the tokens have no columns)
+        groups = (total_q * G + 15 * batch) // 16 * hkv
+        cnt = -(-(n * G) // 16)
+        incl = np.cumsum(cnt)
+        seen = set()
+        for b in range(groups):
+            item, g = b // hkv, b % hkv
+            past = np.flatnonzero(incl > item)
+            if len(past) == 0:
+                continue
+            s = int(past[0])
+            col0 = 16 * (item - int(incl[s] - cnt[s]))
+            cols = min(int(n[s]) * G - col0, 16)
+            assert cols >= 1
+            last = (col0 + cols - 1) // G
+            ctx, rows = int(T[s]) - int(n[s]) + last + 1, last - col0 // G + 1
+            for c in range(16):
+                cc = col0 + min(c, cols - 1)
+                tok = cc // G - col0 // G
+                assert 0 <= tok < rows and ctx - rows + 1 + tok == int(T[s]) - int(n[s]) + cc // G + 1
+                if c < cols:
+                    key = (s, cc // G, g * G + cc % G)
+                    assert key not in seen
+                    seen.add(key)
+        assert len(seen) == int(n.sum()) * G * hkv
