@@ -392,10 +392,24 @@ def window_workspace_size(shape: DecodeShape, window, n_sink=0) -> int:
     return int(lib().window_decode_workspace_size(ctypes.byref(shape), window, n_sink))
 
 
+def _check_window(tensors, shape, k_scale, v_scale) -> None:
+    """Refuses tensors with gaps, and scales that are not the cache type's."""
+    for t in tensors:
+        if not t.is_contiguous():
+            raise ValueError(f"a tensor of strides {tuple(t.stride())} for shape {tuple(t.shape)}: it must be contiguous")
+    if k_scale is not None and v_scale is not None:
+        size = 1 if shape.kv_dtype == KV_FP8_E4M3_BLOCK else 4
+        if k_scale.itemsize != size or v_scale.itemsize != size:
+            raise ValueError("scales are fp32 for each head, or one exponent byte for each block and head")
+        if not (k_scale.is_contiguous() and v_scale.is_contiguous()):
+            raise ValueError("scales must be contiguous")
+
+
 def window_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, scale, window, n_sink, out,
                             shape: DecodeShape, workspace=None, k_scale=None, v_scale=None, stream=None) -> None:
     """Enqueue the decode over a sliding window and the first n_sink tokens, or over block scales
-    (include/dpool.h, window_decode_attention)."""
+    (include/dpool.h, window_decode_attention).  Tensors have to be contiguous (ValueError otherwise)."""
+    _check_window((q, k_blocks, v_blocks, block_tables, out), shape, k_scale, v_scale)
     ws_ptr, ws_bytes = _ws(workspace)
     check(lib().window_decode_attention(
         q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
@@ -435,7 +449,8 @@ def chunked_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens,
 def window_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens, q_start, scale, window, n_sink, out,
                              shape: PrefillShape, k_scale=None, v_scale=None, stream=None) -> None:
     """Enqueue the chunked prefill over a sliding window and the first n_sink tokens, or over block scales
-    (include/dpool.h, window_prefill_attention)."""
+    (include/dpool.h, window_prefill_attention).  Tensors have to be contiguous (ValueError otherwise)."""
+    _check_window((q, k_blocks, v_blocks, block_tables, q_start, out), shape, k_scale, v_scale)
     check(lib().window_prefill_attention(
         q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
         q_start.data_ptr(), float(scale), window, n_sink, k_scale.data_ptr() if k_scale is not None else None,

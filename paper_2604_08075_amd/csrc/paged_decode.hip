@@ -1385,11 +1385,13 @@ template __global__ void paged_decode_small_kernel<true>(DecodeArgs);
 // beside the stream is saved: the search for a slice's units, and the merge of
 // pieces through device-wide memory.  Wave w takes units w, w + 8, w + 16, at most
 // three; one load per lane fetches the table entries of all of them, a shuffle
-// hands them out, and two units are in flight at a time.  More units do not pay
-// (a loop over any number of them, times as below: window 2,048, 32 sequences
-// 35.2 / 35.1, eight 19.2 / 24.0): a compute unit's waves draw about 34 GB/s
-// whatever is in flight, and slices use all 256 units.  Measured, one layer in a
-// replayed graph, us, equal slices / here, 64/8 heads, n_sink 4:
+// hands them out, and two units are in flight at a time.  More units were tried and
+// not kept: a compute unit draws no more than about 36 GB/s, whatever its waves
+// have in flight, and slices use all 256 units.  Four waves with three units in
+// flight, any number of units, e4m3, window 4,096: eight sequences on 64/8 heads
+// 25.7 us in slices / 37.9, 32 sequences 58.2 / 50.4, 32 of mixed lengths 43.8 /
+// 48.8, and the host does not know the lengths.  Measured, one layer in a replayed
+// graph, us, equal slices / here, 64/8 heads, n_sink 4:
 //   bf16, window 512 (18 units)   one sequence 11.7 / 10.6, 16: 17.7 / 13.7, 32:
 //                                 23.7 / 16.8, 32 of mixed lengths 1.31 times
 //   bf16, window 690 (24 units)   one 0.87 times as quick, 8: 0.98, 12: 1.06, 32: 1.27

@@ -156,3 +156,31 @@ def test_append_binding_refuses_gaps(host_lib):
                 dict(q=None, q_out=None, v=torch.zeros((8, 2, 128))[::2])):
         with pytest.raises(ValueError):
             call(**bad)
+
+
+def test_attention_binding_refuses_gaps_and_other_scales(host_lib):
+    import torch
+    q, t = torch.zeros((4, 8, 128), dtype=torch.bfloat16), torch.zeros((4, 100), dtype=torch.int32)
+    k, v = torch.zeros((50, 2, 16, 128), dtype=torch.uint8), torch.zeros((50, 2, 128, 16), dtype=torch.uint8)
+    heads, blocks = torch.zeros(2), torch.zeros((50, 2), dtype=torch.uint8)
+    for scaled, good, bad in ((False, heads, blocks), (True, blocks, heads)):
+        dec = host_lib.decode_shape(4, 8, 2, 100, 1600, 50, kv_fp8=True, block_scales=scaled)
+        pre = host_lib.prefill_shape(4, 8, 2, 100, 1600, 50, 4, kv_fp8=True, block_scales=scaled)
+        d = dict(q=q, k_blocks=k, v_blocks=v, block_tables=t, context_lens=t[0], scale=0.1, window=64, n_sink=0,
+                 out=torch.zeros_like(q), k_scale=good, v_scale=good)
+        for more in (dict(k_scale=bad), dict(v_scale=bad), dict(q=torch.zeros((4, 128, 8)).transpose(1, 2)),
+                     dict(block_tables=torch.zeros((4, 200), dtype=torch.int32)[:, ::2]), dict(k_blocks=k[:, :1]),
+                     dict(out=torch.zeros((4, 9, 128))[:, :8]), dict(v_scale=torch.zeros((50, 4)).to(good.dtype)[:, ::2])):
+            with pytest.raises(ValueError):
+                host_lib.window_decode_attention(**dict(d, **more), shape=dec)
+            with pytest.raises(ValueError):
+                host_lib.window_prefill_attention(**dict(d, **more), q_start=t[0], shape=pre)
+
+
+def test_drafted_trees_refuse_block_scales(host_lib):
+    s = host_lib.tree_shape(2, 8, 2, 100, 1600, 50, 4, kv_fp8=True)
+    s.kv_dtype = host_lib.KV_FP8_E4M3_BLOCK
+    assert host_lib.tree_workspace_size(s) == 0
+    p = (ctypes.c_void_p * 1)(P)
+    o = (ctypes.c_void_p * 1)(2 * P)
+    assert host_lib.lib().kv_cache_accept(p, o, 1, P, P, P, P, P, 4, 3 * P, ctypes.byref(s), None) == ENOTSUP
