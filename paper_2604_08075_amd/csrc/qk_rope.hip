@@ -355,6 +355,10 @@ __device__ __forceinline__ int need_byte(float a) {
   return min(max((int)((__float_as_uint(a) + 0x1fffffu) >> 23) - 8, 1), 246);
 }
 __device__ __forceinline__ float pow2_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+// 1 over it (2^-127 has no exponent byte of its own; a begun block of byte 255 is NaN whatever its codes)
+__device__ __forceinline__ float inverse_pow2_of(int byte) {
+  return byte < 254 ? pow2_of(254 - byte) : __uint_as_float(0x00400000u);
+}
 
 __device__ __forceinline__ float finite_abs(float x) {
   const float b = fabsf(x);
@@ -465,7 +469,7 @@ __device__ __forceinline__ void scaled_part(const RopeArgs& a, int64_t unit, uin
           *(i32x2*)(out + n * kD) = c;
         }
       }
-      const float inv = pow2_of(254 - byte);
+      const float inv = inverse_pow2_of(byte);
       for (int n0 = 0; n0 < len; n0 += 4) {
         const int at_slot = __shfl(slot, f + n0 + sub);
         if (len > 4) turned(n0);
@@ -494,7 +498,7 @@ __device__ __forceinline__ void scaled_part(const RopeArgs& a, int64_t unit, uin
         for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(y[e]));
       }
       const int byte = max(need_byte(wave_max(top)), old);
-      const float inv = pow2_of(254 - byte);
+      const float inv = inverse_pow2_of(byte);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       if (byte != old && off > 0 && len < kBS) {
         const float p = shrink(old, byte);

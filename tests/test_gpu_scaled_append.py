@@ -191,6 +191,17 @@ def test_scales_rise_by_steps_and_limits(gpu_lib):
         check(gpu_lib, rng, slots, pos, nb=80, codes=workloads.to_bf16_codes(x), weights=(False, False), rotary=0)
 
 
+def test_begun_blocks_of_the_largest_scales(gpu_lib):
+    """2^126 and 2^127, whose inverses are the least normal value and below it."""
+    note("scaled append largest scales")
+    rng = np.random.default_rng(55)
+    slots, pos = sequences(rng, [(1 + i % 15, 1 + i % 5) for i in range(30)], 80, 500)
+    x = (rng.standard_normal((len(slots), 8, 128)) * 1e38).clip(-3e38, 3e38).astype(np.float32)
+    for byte in (253, 254):
+        check(gpu_lib, rng, slots, pos, nb=80, codes=workloads.to_bf16_codes(x), byte_range=(byte, byte + 1),
+              weights=(False, False), rotary=0)
+
+
 def test_values_that_are_not_finite(gpu_lib):
     note("scaled append NaN and infinities")
     rng = np.random.default_rng(6)
