@@ -358,10 +358,26 @@ def _stream_ptr(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_here(stream, a, b):
+    """_stream_ptr, for tensors a and b on the current device, where the launch goes; refuses others."""
+    import torch
+    dev = a.get_device()
+    if dev < 0 or dev != b.get_device():
+        raise ValueError(f"tensors on {a.device} and {b.device}: they must be on the current device")
+    try:
+        if dev == torch._C._cuda_getDevice() and stream is None:
+            return torch._C._cuda_getCurrentRawStream(dev)
+    except AttributeError:  # (as in _stream_ptr)
+        pass
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"tensors on {a.device}: they must be on the current device")
+    return _stream_ptr(stream)
+
+
 def _ws(workspace):
     if workspace is None:
         return None, 0
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def paged_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, scale, out, shape: DecodeShape,
@@ -392,11 +408,14 @@ def window_workspace_size(shape: DecodeShape, window, n_sink=0) -> int:
     return int(lib().window_decode_workspace_size(ctypes.byref(shape), window, n_sink))
 
 
-def _check_window(tensors, shape, k_scale, v_scale) -> None:
-    """Refuses tensors with gaps, and scales that are not the cache type's."""
-    for t in tensors:
-        if not t.is_contiguous():
-            raise ValueError(f"a tensor of strides {tuple(t.stride())} for shape {tuple(t.shape)}: it must be contiguous")
+def _check_window(q, k_blocks, v_blocks, block_tables, lens, out, shape, k_scale, v_scale) -> None:
+    """Refuses tensors with gaps, ids that are not int32, scales that are not the cache type's."""
+    # (written out: half of what a loop takes on the host, 0.6 us)
+    if not (q.is_contiguous() and k_blocks.is_contiguous() and v_blocks.is_contiguous() and block_tables.is_contiguous()
+            and lens.is_contiguous() and out.is_contiguous()):
+        raise ValueError("q, caches, block tables, lengths and out must be contiguous")
+    if block_tables.itemsize != 4 or lens.itemsize != 4:
+        raise ValueError("block tables and lengths are int32")
     if k_scale is not None and v_scale is not None:
         size = 1 if shape.kv_dtype == KV_FP8_E4M3_BLOCK else 4
         if k_scale.itemsize != size or v_scale.itemsize != size:
@@ -408,14 +427,15 @@ def _check_window(tensors, shape, k_scale, v_scale) -> None:
 def window_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, scale, window, n_sink, out,
                             shape: DecodeShape, workspace=None, k_scale=None, v_scale=None, stream=None) -> None:
     """Enqueue the decode over a sliding window and the first n_sink tokens, or over block scales
-    (include/dpool.h, window_decode_attention).  Tensors have to be contiguous (ValueError otherwise)."""
-    _check_window((q, k_blocks, v_blocks, block_tables, out), shape, k_scale, v_scale)
+    (include/dpool.h, window_decode_attention).  Tensors have to be contiguous and on the
+    current device (ValueError otherwise)."""
+    _check_window(q, k_blocks, v_blocks, block_tables, context_lens, out, shape, k_scale, v_scale)
     ws_ptr, ws_bytes = _ws(workspace)
     check(lib().window_decode_attention(
         q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
         float(scale), window, n_sink, k_scale.data_ptr() if k_scale is not None else None,
         v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape), ws_ptr, ws_bytes,
-        _stream_ptr(stream)))
+        _stream_here(stream, q, k_blocks)))
 
 
 def kv_cache_append(k_new, v_new, k_blocks, v_blocks, block_tables, positions, shape: DecodeShape, k_scale=None,
@@ -449,13 +469,16 @@ def chunked_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens,
 def window_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens, q_start, scale, window, n_sink, out,
                              shape: PrefillShape, k_scale=None, v_scale=None, stream=None) -> None:
     """Enqueue the chunked prefill over a sliding window and the first n_sink tokens, or over block scales
-    (include/dpool.h, window_prefill_attention).  Tensors have to be contiguous (ValueError otherwise)."""
-    _check_window((q, k_blocks, v_blocks, block_tables, q_start, out), shape, k_scale, v_scale)
+    (include/dpool.h, window_prefill_attention).  Tensors have to be contiguous and on the
+    current device (ValueError otherwise)."""
+    _check_window(q, k_blocks, v_blocks, block_tables, context_lens, out, shape, k_scale, v_scale)
+    if not q_start.is_contiguous() or q_start.itemsize != 4:
+        raise ValueError("q_start is int32 and contiguous")
     check(lib().window_prefill_attention(
         q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
         q_start.data_ptr(), float(scale), window, n_sink, k_scale.data_ptr() if k_scale is not None else None,
         v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape),
-        _stream_ptr(stream)))
+        _stream_here(stream, q, k_blocks)))
 
 
 # ---------------------------------------------------------------- a step that verifies drafted tokens
@@ -537,23 +560,26 @@ def qk_norm_rope_append_scaled(q, k, v, cos_sin, positions, slots, q_out, k_bloc
     qk_norm_rope_append_scaled); k_scale and v_scale, one byte each, are updated with it.
 
     q and q_out may be None where the shape has no query heads.  Rows as for
-    qk_norm_rope_append; caches and scales have to be contiguous (ValueError)."""
+    qk_norm_rope_append; caches, scales, positions and slots have to be
+    contiguous and on the current device (ValueError)."""
     if q is None:
         _check_rows("k", k, shape.rows, shape.n_kv_heads, shape.head_dim, shape.k_stride)
         _check_rows("v", v, shape.rows, shape.n_kv_heads, shape.head_dim, shape.v_stride)
     else:
         _check_qkv(q, k, v, q_out, shape)
     if not (k_blocks.is_contiguous() and v_blocks.is_contiguous() and k_scale.is_contiguous()
-            and v_scale.is_contiguous()):
-        raise ValueError("caches and scales must be contiguous")
+            and v_scale.is_contiguous() and positions.is_contiguous() and slots.is_contiguous()):
+        raise ValueError("caches, scales, positions and slots must be contiguous")
     if k_scale.itemsize != 1 or v_scale.itemsize != 1:
         raise ValueError("k_scale and v_scale hold one exponent byte for each block and head")
+    if positions.itemsize != 4 or slots.itemsize != 8:
+        raise ValueError("positions are int32, slots int64")
     check(lib().qk_norm_rope_append_scaled(
         q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(),
         q_weight.data_ptr() if q_weight is not None else None, k_weight.data_ptr() if k_weight is not None else None,
         float(eps), cos_sin.data_ptr() if cos_sin is not None else None, positions.data_ptr(), slots.data_ptr(),
         q_out.data_ptr() if q_out is not None else None, k_blocks.data_ptr(), v_blocks.data_ptr(), k_scale.data_ptr(),
-        v_scale.data_ptr(), ctypes.byref(shape), _stream_ptr(stream)))
+        v_scale.data_ptr(), ctypes.byref(shape), _stream_here(stream, k, k_blocks)))
 
 
 def tree_shape(batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks, total_q, mask_words=1,

@@ -210,3 +210,17 @@ def test_nothing_cached(gpu_lib, fmt, batch):
     note(f"window decode {fmt} empty sequences batch={batch}")
     c = Case(np.random.default_rng(14), [0] * batch, None, 4, 1, fmt, 10, 2)
     assert (wc.decode(gpu_lib, c) == 0).all() and (wc.decode(gpu_lib, c, max_ctx=16) == 0).all()
+
+
+def test_tensors_that_are_elsewhere(gpu_lib):
+    """A queries' tensor or a cache in host memory is refused before anything is enqueued."""
+    note("window decode, host tensors")
+    c = Case(np.random.default_rng(12), [40], None, 4, 2, "bf16", 16, 0)
+    d = c.device()
+    for name in ("q", "k"):
+        with pytest.raises(ValueError):
+            wc.decode(gpu_lib, c, d=dict(d, **{name: d[name].cpu()}))
+    p = Case(np.random.default_rng(12), [40], [3], 4, 2, "bf16", 16, 0)
+    d = p.device()
+    with pytest.raises(ValueError):
+        wc.prefill(gpu_lib, p, d=dict(d, k=d["k"].cpu()))

@@ -153,12 +153,14 @@ def test_append_binding_refuses_gaps(host_lib):
     for bad in (dict(q_out=torch.zeros((4, 9, 128), dtype=torch.bfloat16)[:, :8]), dict(k=torch.zeros((8, 2, 128))[::2]),
                 dict(k_blocks=torch.zeros((64, 4, 16, 128), dtype=torch.uint8)[:, ::2]),
                 dict(v_scale=torch.zeros((64, 4), dtype=torch.uint8)[:, :2]), dict(k_scale=torch.zeros(64, 2)),
-                dict(q=None, q_out=None, v=torch.zeros((8, 2, 128))[::2])):
+                dict(q=None, q_out=None, v=torch.zeros((8, 2, 128))[::2]), dict(slots=i.int()), dict(positions=i),
+                dict(slots=torch.zeros(8, dtype=torch.int64)[::2]), dict(positions=torch.zeros(8).int()[::2]),
+                dict()):  # (nothing but that the tensors are not on a device)
         with pytest.raises(ValueError):
             call(**bad)
 
 
-def test_attention_binding_refuses_gaps_and_other_scales(host_lib):
+def test_attention_binding_refuses_gaps_and_other_types(host_lib):
     import torch
     q, t = torch.zeros((4, 8, 128), dtype=torch.bfloat16), torch.zeros((4, 100), dtype=torch.int32)
     k, v = torch.zeros((50, 2, 16, 128), dtype=torch.uint8), torch.zeros((50, 2, 128, 16), dtype=torch.uint8)
@@ -170,11 +172,15 @@ def test_attention_binding_refuses_gaps_and_other_scales(host_lib):
                  out=torch.zeros_like(q), k_scale=good, v_scale=good)
         for more in (dict(k_scale=bad), dict(v_scale=bad), dict(q=torch.zeros((4, 128, 8)).transpose(1, 2)),
                      dict(block_tables=torch.zeros((4, 200), dtype=torch.int32)[:, ::2]), dict(k_blocks=k[:, :1]),
-                     dict(out=torch.zeros((4, 9, 128))[:, :8]), dict(v_scale=torch.zeros((50, 4)).to(good.dtype)[:, ::2])):
+                     dict(out=torch.zeros((4, 9, 128))[:, :8]), dict(v_scale=torch.zeros((50, 4)).to(good.dtype)[:, ::2]),
+                     dict(context_lens=t[0].long()), dict(block_tables=t.long()), dict(context_lens=t[:, 0]), dict()):
             with pytest.raises(ValueError):
                 host_lib.window_decode_attention(**dict(d, **more), shape=dec)
             with pytest.raises(ValueError):
                 host_lib.window_prefill_attention(**dict(d, **more), q_start=t[0], shape=pre)
+        for start in (t[0].long(), t[:, 0]):
+            with pytest.raises(ValueError):
+                host_lib.window_prefill_attention(**d, q_start=start, shape=pre)
 
 
 def test_drafted_trees_refuse_block_scales(host_lib):
