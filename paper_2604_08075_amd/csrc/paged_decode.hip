@@ -487,6 +487,17 @@ __device__ __forceinline__ int wave_incl_scan(int x) {
   return x;
 }
 
+// Maximum over the 64 lanes, by the same moves (a lane with no source keeps its own).
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
 // A workgroup barrier that waits for LDS accesses only, not for loads or
 // stores to memory still in flight.
 __device__ __forceinline__ void lds_barrier() {
@@ -648,6 +659,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
   constexpr int UB = GE::UB, UT = GE::UT, TILE = GE::TILE;
   __shared__ int tiles_lds[kWaves][kMaxUnitsPerWave * UB];
   __shared__ int wave_sums[kWaves];
+  __shared__ int wave_segs[WIN ? kWaves : 1][3];  // sequences with units, the most and the least units of one
   // Split pieces are first merged inside the workgroup: the segment (s, g)
   // of each wave's first and last split piece (s = -1: none).
   __shared__ int wg_seg[2 * kWaves][2];
@@ -696,6 +708,27 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
   UnitRegs RA;
 
   // ---- 1. prefix of units over sequences ----
+  const int TW = gridDim.x * kWaves;
+  // (WIN) Windows make segments alike.  Where four, two or one slice to a segment
+  // are about as long as equal slices would be, each segment takes whole slices, the
+  // last of them shorter, and nothing is left to merge across workgroups.  One layer
+  // in a replayed graph, us, equal slices / segments apart: e4m3, window 4,096, 64
+  // sequences on 64/4 heads 53.6 / 50.1; bf16, window 1,024, 32 on 64/8 35.8 / 32.6;
+  // e4m3, window 2,048, 64 of 1,700 to 2,048 tokens on 64/4 31.3 / 28.1; two segments
+  // to a workgroup (block scales, 64 on 64/8) 35.7 / 34.2; one to a wave (bf16, 128 on
+  // 64/8) 89.1 / 87.0.  Lengths of all kinds pay 0.2 for the question.
+  int apart = 0, lg_slices = 0;  // units of a slice (0: equal slices), and log2 of the slices of a segment
+  constexpr int kNone = 1 << 30;
+  auto lay_apart = [&](int live, int longest, int shortest, int units) __attribute__((always_inline)) {
+    const int n = gridDim.x, segs = Hkv * live, C = max((Hkv * units + TW - 1) / TW, a.min_chunk);
+    const int lg = segs <= n ? 2 : segs <= 2 * n ? 1 : 0;
+    const int slice = (longest + (1 << lg) - 1) >> lg;
+    if (longest > 0 && segs << lg <= TW && shortest > slice * ((1 << lg) - 1) && slice >= a.min_chunk &&
+        slice <= min(C + 1 + (C >> 4), kMaxUnitsPerWave)) {
+      apart = slice;
+      lg_slices = lg;
+    }
+  };
   if (B <= 64) {
     // Every wave computes all of it, one sequence a lane: the four waves write
     // the same values, each reads only what it wrote itself (a wave's LDS
@@ -711,7 +744,13 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
     int c = clamp_ctx(a.context_lens[min(lane, B - 1)], a.max_ctx);
     if (lane >= B) c = 0;
     issue_at(RA, ck, cv);
-    const int incl = wave_incl_scan(live_span<FP8, WIN>(a, c).nus);
+    int nus = live_span<FP8, WIN>(a, c).nus;
+    int incl = wave_incl_scan(nus);
+    if constexpr (WIN) {
+      lay_apart(__popcll(__ballot(nus > 0)), wave_max(nus), -wave_max(nus ? -nus : -kNone),
+                __builtin_amdgcn_readlane(incl, 63));
+      if (apart) incl = wave_incl_scan(nus > 0 ? apart << lg_slices : 0);
+    }
     if (lane < B) {
       ctxs[lane] = c;
       pre[lane + 1] = incl;
@@ -728,35 +767,65 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
       }
     }
     const int per = (B + T - 1) / T;
-    int local = 0;
+    int local = 0, live = 0, longest = 0, shortest = kNone;
     for (int k = 0; k < per; ++k) {
       const int s = tid * per + k;
       if (s < B) {
         const int c = clamp_ctx(a.context_lens[s], a.max_ctx);
         ctxs[s] = c;
-        local += live_span<FP8, WIN>(a, c).nus;
+        const int nus = live_span<FP8, WIN>(a, c).nus;
+        local += nus;
+        if (WIN && nus > 0) {
+          ++live;
+          longest = max(longest, nus);
+          shortest = min(shortest, nus);
+        }
       }
     }
     issue_at(RA, ck, cv);
     const int incl = wave_incl_scan(local);
     if (lane == 63) wave_sums[w] = incl;
+    int lives = 0;
+    if constexpr (WIN) {
+      lives = wave_incl_scan(live);
+      longest = wave_max(longest);
+      shortest = -wave_max(-shortest);
+      if (lane == 63) {
+        wave_segs[w][0] = lives;
+        wave_segs[w][1] = longest;
+        wave_segs[w][2] = shortest;
+      }
+    }
     lds_barrier();  // (LDS only: the first unit's loads stay in flight)
     int run = incl - local;
     for (int k = 0; k < w; ++k) run += wave_sums[k];
+    if constexpr (WIN) {
+      int units = 0, all = 0, before = lives - live;
+      for (int k = 0; k < kWaves; ++k) {
+        units += wave_sums[k];
+        all += wave_segs[k][0];
+        if (k < w) before += wave_segs[k][0];
+        longest = max(longest, wave_segs[k][1]);
+        shortest = min(shortest, wave_segs[k][2]);
+      }
+      lay_apart(all, longest, shortest, units);
+      if (apart) run = before * (apart << lg_slices);
+    }
     for (int k = 0; k < per; ++k) {
       const int s = tid * per + k;
       if (s < B) {
         pre[s] = run;
-        run += live_span<FP8, WIN>(a, ctxs[s]).nus;
+        const int nus = live_span<FP8, WIN>(a, ctxs[s]).nus;
+        run += WIN && apart && nus > 0 ? apart << lg_slices : nus;
       }
     }
     if (tid == T - 1) pre[B] = run;
     lds_barrier();
   }
   const int U = Hkv * pre[B];
-  const int TW = gridDim.x * kWaves;
   int C = (U + TW - 1) / TW;
   if (C < a.min_chunk) C = a.min_chunk;
+  if (WIN && apart) C = apart;
   const float rC = 1.0f / (float)C, rCW = 1.0f / (float)(kWaves * C);  // for the merge's slice arithmetic
 
   // rows of empty sequences are zero
@@ -776,7 +845,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
   // split segments this wave must signal: (s, g) of its first piece and of its last piece, s = -1 if none
   int arr_s0 = -1, arr_g0 = 0, arr_s1 = -1, arr_g1 = 0;
   if (u0 < u1) {  // a wave without units goes straight to the merge
-    const int n = u1 - u0;
+    int n = u1 - u0;
 
     // ---- 2. tile indices (block id * Hkv + head) of this wave's units ----
     int* tiles = tiles_lds[w];
@@ -794,15 +863,15 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
       const int r = u - Hkv * pre[s];
       const int g = r / nus;
       const int j = r - g * nus;
+      const int nb = (ctxs[s] + kBlock - 1) / kBlock;
+      const Span sp = live_span<FP8, WIN>(a, ctxs[s]);
       if (i == lane) {
         f_s = s;
-        f_nus = nus;
+        f_nus = WIN ? sp.nus : nus;
         f_g = g;
         f_j = j;
       }
-      const int nb = (ctxs[s] + kBlock - 1) / kBlock;
-      const Span sp = live_span<FP8, WIN>(a, ctxs[s]);
-      const int jr = real_unit<WIN>(sp, j);
+      const int jr = real_unit<WIN>(sp, WIN ? min(j, sp.nus - 1) : j);
       for (int b = 0; b < UB; ++b) {
         const int blk = live_block<FP8, WIN>(a, sp, jr, b, nb);
         int id = a.block_tables[(size_t)s * a.max_blocks_per_seq + blk];
@@ -827,6 +896,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
     cs.nus = __builtin_amdgcn_readlane(f_nus, 0);
     cs.g = __builtin_amdgcn_readlane(f_g, 0);
     cs.j = __builtin_amdgcn_readlane(f_j, 0);
+    if (WIN && apart) n = min(n, cs.nus - cs.j);
     auto advance = [&](Walker& wk) __attribute__((always_inline)) {
       if (++wk.j == wk.nus) {
         wk.j = 0;
@@ -1698,7 +1768,7 @@ int validate(const dp_decode_shape* sh, const Window* win, Plan* plan) {
   plan->variant = win ? 2 + sh->kv_dtype : sh->kv_dtype;
   // LDS per workgroup: the kernel's static arrays (tile lists, wave sums,
   // each wave's two records, the workgroup's merge counters, with 256 bytes
-  // for alignment) +
+  // for alignment and, with a window, 48 for wave_segs) +
   // unit prefix, context lengths and fp8 scales (dynamic)
   const size_t stat = (size_t)kWaves * kMaxUnitsPerWave * (fp8 ? 4 : 2) * sizeof(int) + kWaves * sizeof(int) +
                       (size_t)kWaves * 2 * kRecBytes + (size_t)4 * kWaves * sizeof(int) + 256;

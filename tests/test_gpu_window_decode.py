@@ -224,3 +224,26 @@ def test_tensors_that_are_elsewhere(gpu_lib):
     d = p.device()
     with pytest.raises(ValueError):
         wc.prefill(gpu_lib, p, d=dict(d, k=d["k"].cpu()))
+
+
+@pytest.mark.parametrize("batch,hkv", [(6, 2), (64, 1), (70, 2), (300, 1)])
+@pytest.mark.parametrize("lg", [2, 1, 0])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_segments_apart(gpu_lib, fmt, lg, batch, hkv):
+    """Segments of seven or eight units over as many workgroups, half or a quarter as many: each takes four, two or
+    one slice of its own.  Then one segment too short for its slices among them, and empty ones."""
+    note(f"window decode {fmt} segments apart lg={lg} batch={batch}")
+    rng = np.random.default_rng(13)
+    unit = 32 if fmt == "bf16" else 64
+    kw = dict(max_ctx=9 * unit, partition_tokens=unit * (8 >> lg))
+    lens = [rng.integers(7 * unit, 9 * unit + 1, batch)]
+    lens.append(np.where(rng.random(batch) < 0.2, 0, lens[0]))
+    lens.append(lens[1].copy())
+    lens[2][batch // 2] = unit // 2
+    lens.append(np.where(np.arange(batch) == batch - 1, lens[0], 0))
+    for ctx in lens:
+        c = Case(rng, ctx, None, 4 * hkv, hkv, fmt, 7 * unit, 0, max_blocks=9 * unit // 16)
+        d = c.device()
+        out = wc.decode(gpu_lib, c, d=d, **kw)
+        wc.check(out, *c.oracle())
+        assert torch.equal(out, wc.decode(gpu_lib, c, d=d, **kw))
