@@ -709,24 +709,32 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
 
   // ---- 1. prefix of units over sequences ----
   const int TW = gridDim.x * kWaves;
-  // (WIN) Windows make segments alike.  Where four, two or one slice to a segment
-  // are about as long as equal slices would be, each segment takes whole slices, the
-  // last of them shorter, and nothing is left to merge across workgroups.  One layer
-  // in a replayed graph, us, equal slices / segments apart: e4m3, window 4,096, 64
-  // sequences on 64/4 heads 53.6 / 50.1; bf16, window 1,024, 32 on 64/8 35.8 / 32.6;
-  // e4m3, window 2,048, 64 of 1,700 to 2,048 tokens on 64/4 31.3 / 28.1; two segments
-  // to a workgroup (block scales, 64 on 64/8) 35.7 / 34.2; one to a wave (bf16, 128 on
-  // 64/8) 89.1 / 87.0.  Lengths of all kinds pay 0.2 for the question.
-  int apart = 0, lg_slices = 0;  // units of a slice (0: equal slices), and log2 of the slices of a segment
+  // (WIN) Windows make segments alike.  Where one, two, four or eight slices to a
+  // segment are about as long as equal slices would be, each segment takes whole
+  // slices, its last one shorter: nothing is left to merge across workgroups, or a
+  // segment's two workgroups share no other's.  One layer in a replayed graph, us,
+  // equal slices / segments apart: e4m3, window 4,096, 64 sequences on 64/4 heads
+  // 53.6 / 50.1; bf16, window 1,024, 32 on 64/8 35.8 / 32.6; e4m3, window 2,048, 64 of
+  // 1,700 to 2,048 tokens on 64/4 31.3 / 28.1; two segments to a workgroup (block
+  // scales, 64 on 64/8) 35.7 / 34.2; one to a wave (bf16, 128 on 64/8) 89.1 / 87.0;
+  // two workgroups to a segment (block scales, window 2,048, 16 on 64/8) 21.7 / 19.8.
+  // Four or more to a segment gained nothing (33.0 / 33.3, 30.1 / 29.8).  Lengths of
+  // all kinds pay 0.2 for the question.
+  int apart = 0, lg_slices = 0;  // units of such a slice (0: equal slices), log2 of the slices of a segment,
+  int used = 0;                  // and how many of those hold units
+  int C = 0;                     // units of a slice
   constexpr int kNone = 1 << 30;
   auto lay_apart = [&](int live, int longest, int shortest, int units) __attribute__((always_inline)) {
-    const int n = gridDim.x, segs = Hkv * live, C = max((Hkv * units + TW - 1) / TW, a.min_chunk);
-    const int lg = segs <= n ? 2 : segs <= 2 * n ? 1 : 0;
+    C = max((Hkv * units + TW - 1) / TW, a.min_chunk);
+    const int segs = Hkv * live;
+    if (longest == 0 || segs > TW) return;
+    const int lg = 8 * segs <= TW ? 3 : 4 * segs <= TW ? 2 : 2 * segs <= TW ? 1 : 0;
     const int slice = (longest + (1 << lg) - 1) >> lg;
-    if (longest > 0 && segs << lg <= TW && shortest > slice * ((1 << lg) - 1) && slice >= a.min_chunk &&
-        slice <= min(C + 1 + (C >> 4), kMaxUnitsPerWave)) {
-      apart = slice;
+    const int last = div_small(longest - 1, slice, __builtin_amdgcn_rcpf((float)slice));  // (below eight)
+    if (shortest > slice * last && slice >= a.min_chunk && slice <= min(C + 1 + (C >> 4), kMaxUnitsPerWave)) {
+      apart = C = slice;
       lg_slices = lg;
+      used = last + 1;
     }
   };
   if (B <= 64) {
@@ -823,9 +831,10 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
     lds_barrier();
   }
   const int U = Hkv * pre[B];
-  int C = (U + TW - 1) / TW;
-  if (C < a.min_chunk) C = a.min_chunk;
-  if (WIN && apart) C = apart;
+  if constexpr (!WIN) {
+    C = (U + TW - 1) / TW;
+    if (C < a.min_chunk) C = a.min_chunk;
+  }
   const float rC = 1.0f / (float)C, rCW = 1.0f / (float)(kWaves * C);  // for the merge's slice arithmetic
 
   // rows of empty sequences are zero
@@ -844,7 +853,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
   const int u1 = min(u0 + C, U);
   // split segments this wave must signal: (s, g) of its first piece and of its last piece, s = -1 if none
   int arr_s0 = -1, arr_g0 = 0, arr_s1 = -1, arr_g1 = 0;
-  if (u0 < u1) {  // a wave without units goes straight to the merge
+  if (u0 < u1 && !(WIN && apart && (gw & ((1 << lg_slices) - 1)) >= used)) {  // a wave without units goes straight to the merge
     int n = u1 - u0;
 
     // ---- 2. tile indices (block id * Hkv + head) of this wave's units ----
@@ -1090,15 +1099,16 @@ __global__ __launch_bounds__(kWaves * 64) void paged_decode_kernel(DecodeArgs a)
     // the same for the whole wave: scalar registers, scalar branches
     const int nus = __builtin_amdgcn_readfirstlane(pre[s + 1] - pre[s]);
     const int a0 = __builtin_amdgcn_readfirstlane(Hkv * pre[s] + g * nus);  // first unit of the segment
+    const int taken = WIN && apart ? used * apart : nus;
     p.s = s;
     p.g = g;
     p.k0 = div_small(a0, C, rC);
-    const int kend = div_small(a0 + nus - 1, C, rC);
+    const int kend = div_small(a0 + taken - 1, C, rC);
     p.first_slot = 2 * p.k0 + (a0 > p.k0 * C ? 1 : 0);
     p.pk0 = max(p.k0, wg_first);
     p.pkend = min(kend, wg_first + kWaves - 1);
     p.bk0 = div_small(a0, CW, rCW);
-    p.bkend = div_small(a0 + nus - 1, CW, rCW);
+    p.bkend = div_small(a0 + taken - 1, CW, rCW);
     p.nwp = p.bkend - p.bk0 + 1;
     p.first_wslot = 2 * p.bk0 + (a0 > p.bk0 * CW ? 1 : 0);
     p.rb = (int)blockIdx.x - p.bk0;

@@ -227,11 +227,11 @@ def test_tensors_that_are_elsewhere(gpu_lib):
 
 
 @pytest.mark.parametrize("batch,hkv", [(6, 2), (64, 1), (70, 2), (300, 1)])
-@pytest.mark.parametrize("lg", [2, 1, 0])
+@pytest.mark.parametrize("lg", [3, 2, 1, 0])
 @pytest.mark.parametrize("fmt", FMTS)
 def test_segments_apart(gpu_lib, fmt, lg, batch, hkv):
-    """Segments of seven or eight units over as many workgroups, half or a quarter as many: each takes four, two or
-    one slice of its own.  Then one segment too short for its slices among them, and empty ones."""
+    """Segments of seven or eight units over twice as many workgroups, as many, half or a quarter as many: each takes
+    eight, four, two or one slice of its own (300 over the 256 of a device two at most).  Then one segment too short for its slices among them, and empty ones."""
     note(f"window decode {fmt} segments apart lg={lg} batch={batch}")
     rng = np.random.default_rng(13)
     unit = 32 if fmt == "bf16" else 64

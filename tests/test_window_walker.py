@@ -14,8 +14,8 @@ attend_unit, and checks against the definition that
   * where a segment is one workgroup's, its eight waves take every unit once, at
     most three each;
   * where segments are laid apart, every slice is part of one segment, the
-    slices of a segment belong to one workgroup, each has a unit, and together
-    they take every unit once;
+    slices of a segment belong to one workgroup (to two, where they are eight),
+    those in use have a unit each, and together they take every unit once;
   * the prefill kernel's items: their steps hold every token that one of their
     rows sees, block ids are staged for those alone and from entries of blocks
     that a row sees, a wave calls a tile hidden exactly if none of its columns
@@ -81,27 +81,28 @@ def test_units_blocks_and_masks(ut):
 
 
 def lay_apart(nus, hkv, groups, waves, min_chunk, most):
-    """(units of a slice, log2 of the slices of a segment), (0, 0) for equal slices."""
+    """(units of a slice, log2 of the slices of a segment, slices in use), zeros for equal slices."""
     live = [n for n in nus if n > 0]
     segs, c = hkv * len(live), max(-(-hkv * sum(nus) // (groups * waves)), min_chunk)
-    lg = 2 if segs <= groups else 1 if segs <= 2 * groups else 0
-    longest, shortest = max(live, default=0), min(live, default=1 << 30)
-    slice_ = (longest + (1 << lg) - 1) >> lg
-    if longest > 0 and segs << lg <= groups * waves and shortest > slice_ * ((1 << lg) - 1) and slice_ >= min_chunk and \
-            slice_ <= min(c + 1 + (c >> 4), most):
-        return slice_, lg
-    return 0, 0
+    if not live or segs > groups * waves:
+        return 0, 0, 0
+    lg = min((groups * waves // segs).bit_length() - 1, 3)
+    slice_ = (max(live) + (1 << lg) - 1) >> lg
+    last = (max(live) - 1) // slice_
+    if min(live) > slice_ * last and slice_ >= min_chunk and slice_ <= min(c + 1 + (c >> 4), most):
+        return slice_, lg, last + 1
+    return 0, 0, 0
 
 
 def test_segments_apart():
     rng = np.random.default_rng(3)
-    waves, most, seen = 4, 256, [0, 0, 0]
+    waves, most, seen = 4, 256, [0, 0, 0, 0]
     for _ in range(3000):
         hkv, groups = int(rng.integers(1, 9)), int(rng.choice([1, 3, 16, 64, 256]))
         base, spread = int(rng.integers(1, 80)), int(rng.integers(0, 8))
         nus = [int(x) for x in rng.integers(max(base - spread, 1), base + 1, int(rng.integers(1, 80)))]
         nus = [0 if rng.random() < 0.1 else n for n in nus]
-        c, lg = lay_apart(nus, hkv, groups, waves, int(rng.choice([1, 1, 2, 8])), most)
+        c, lg, used = lay_apart(nus, hkv, groups, waves, int(rng.choice([1, 1, 2, 8])), most)
         if c == 0:
             continue
         seen[lg] += 1
@@ -111,7 +112,7 @@ def test_segments_apart():
         took = {}
         for gw in range(groups * waves):
             u0, u1 = gw * c, min(gw * c + c, total)
-            if u0 >= u1:
+            if u0 >= u1 or gw % (1 << lg) >= used:
                 continue
             s = max(i for i in range(len(nus)) if hkv * pre[i] <= u0)
             vnus = int(pre[s + 1] - pre[s])
@@ -123,9 +124,9 @@ def test_segments_apart():
         for (s, g), parts in took.items():
             assert [j for _, r in parts for j in r] == list(range(nus[s]))
             a0 = hkv * int(pre[s]) + g * (c << lg)
-            k0, kend = a0 // c, (a0 + (c << lg) - 1) // c
+            k0, kend = a0 // c, (a0 + used * c - 1) // c
             assert [gw for gw, _ in parts] == list(range(k0, kend + 1)) and a0 == k0 * c
-            assert k0 // waves == kend // waves
+            assert kend // waves - k0 // waves <= (1 if lg == 3 else 0)
     assert min(seen) > 20, seen
 
 
