@@ -1471,12 +1471,18 @@ template __global__ void paged_decode_small_kernel<true>(DecodeArgs);
 // flight, any number of units, e4m3, window 4,096: eight sequences on 64/8 heads
 // 25.7 us in slices / 37.9, 32 sequences 58.2 / 50.4, 32 of mixed lengths 43.8 /
 // 48.8, and the host does not know the lengths.  Measured, one layer in a replayed
-// graph, us, equal slices / here, 64/8 heads, n_sink 4:
-//   bf16, window 512 (18 units)   one sequence 11.7 / 10.6, 16: 17.7 / 13.7, 32:
-//                                 23.7 / 16.8, 32 of mixed lengths 1.31 times
-//   bf16, window 690 (24 units)   one 0.87 times as quick, 8: 0.98, 12: 1.06, 32: 1.27
-//   e4m3, window 1,024 (18 units) one 1.04 times, 16: 18.9 / 14.9, 32: 24.2 / 17.2
-//   block scales, window 1,024    one 1.00 times, 16: 18.7 / 16.0, 32: 24.4 / 19.0
+// graph, us, slices / here, full windows, 64/8 heads, n_sink 4 (slices of segments
+// that lie apart, where there are many):
+//   bf16, window 512 (18 units)     one sequence 10.6 / 9.8, 16: 14.0 / 13.3, 32: 17.3 / 15.2,
+//                                   32 of mixed lengths 17.2 / 13.5
+//   e4m3, window 1,024 (18 units)   one 11.7 / 11.7, 16: 15.6 / 14.1, 32: 18.4 / 15.6
+//   block scales, window 1,024      one 11.4 / 11.9, four 12.2 / 13.4, 16: 15.5 / 15.2, 32: 18.4 / 17.3
+//   bf16, window 690 (24 units)     12 sequences 15.1 / 15.2 (mixed 13.3 / 14.7), 16: 15.7 / 15.7
+//                                   (15.8 / 15.1), 32: 20.1 / 18.5
+//   e4m3, window 1,400 (24 units)   12: 16.7 / 16.2 (15.5 / 15.9), 16: 17.2 / 16.9 (17.3 / 16.0), 32: 21.7 / 19.5
+//   block scales, window 1,400      16: 17.0 / 18.4 (17.1 / 17.7), 24: 20.4 / 19.3 (17.8 / 18.2), 32: 21.8 / 21.0
+// so that more than 18 units are taken from half as many segments as compute units
+// on, with block scales from five eighths.
 // Against two whole units a wave on maxima of their own, their entries loaded for
 // K and V apart (paged_decode_small_kernel's way): bf16, window 64, one sequence
 // 6.4 / 5.5, window 256, 32 sequences 13.8 / 10.7.
@@ -1798,9 +1804,11 @@ int validate(const dp_decode_shape* sh, const Window* win, Plan* plan) {
   plan->grid = (int)grid;
   // (why the lines lie here: at paged_decode_small_kernel and window_decode_kernel)
   const int64_t segments = (int64_t)sh->batch * sh->n_kv_heads;
+  const bool blk = sh->kv_dtype == DP_KV_FP8_E4M3_BLOCK;
   plan->whole = P == 0 && wpc == 0 && segments <= cus &&
                 (units_per_seq <= kSmallUnits ||
-                 (win && (units_per_seq <= kSmallUnits + 2 || (units_per_seq <= kWholeUnits && 8 * segments >= 3 * cus))));
+                 (win && (units_per_seq <= kSmallUnits + 2 ||
+                          (units_per_seq <= kWholeUnits && 8 * segments >= (blk ? 5 : 4) * cus))));
   const int G = sh->n_q_heads / sh->n_kv_heads;
   const size_t waves = (size_t)grid * kWaves;
   // The arrival counters open the workspace, and every call returns the ones

@@ -182,9 +182,10 @@ def test_scale_bytes_over_the_range(gpu_lib, byte):
 
 
 # one workgroup a segment: one to three units a wave, up to one segment a compute unit, at the
-# lines of the rule (18 units at any batch, 24 from 96 segments on 256 units) and past them
+# lines of the rule (18 units at any batch, 24 from 128 segments on 256 compute units, with block
+# scales from 160) and past them
 @pytest.mark.parametrize("fmt", FMTS)
-@pytest.mark.parametrize("batch,hkv", [(1, 1), (12, 8), (32, 8), (33, 8), (96, 1)])
+@pytest.mark.parametrize("batch,hkv", [(1, 1), (12, 8), (16, 8), (20, 8), (32, 8), (33, 8), (96, 1)])
 @pytest.mark.parametrize("units", [1, 8, 9, 16, 17, 18, 19, 22])
 def test_units_a_wave(gpu_lib, fmt, batch, hkv, units):
     note(f"window decode {fmt} batch={batch} heads={hkv} units={units}")
