@@ -559,7 +559,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     auto vread = [&](const char* base, int nn) __attribute__((always_inline)) {
       return *(const i32x4*)(base + (32 * kVPitch + 128) * (nn >> 1) + 4 * kVPitch * (nn & 1));
     };
-    auto vfrag = [&](int slot, int nn) __attribute__((always_inline)) { return vread(vbase(slot), nn); };
+    // V of tile j, which is in `slot`: zeros where the wave sees nothing of it
+    auto vtile = [&](int j, int slot) __attribute__((always_inline)) {
+      return hidden(j) ? (const char*)zero_v : vbase(slot);
+    };
     struct Scores { f32x4 z[NC][2]; };       // [column block][m]: tokens 8 lj + 4 m + e
     struct Probs { i32x4 p[NC]; };
     // S^T += K Q^T: row group and 32-dim chunk f, column block b
@@ -676,7 +679,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
                     __attribute__((always_inline)) {
 #pragma unroll
       for (int f = 0; f < 4; ++f) kf[f] = kfrag(par ^ 1, f);
-      const char* const vb = hidden(j - 1) ? (const char*)zero_v : vbase(par ^ 1);
+      const char* const vb = vtile(j - 1, par ^ 1);
       bool grown = false;
       if (j >= j_rare || (WIN && j < j_left) || __builtin_amdgcn_ballot_w64(over > 0.f) != 0) {
         grown = prepare(j, cur);
@@ -781,8 +784,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
 #pragma unroll
       for (int b = 0; b < NC; ++b) pB.p[b] = pA.p[b];
     }
+    const char* const last = vtile(nt_w - 1, (nt_w & 1) ^ 1);  // (nt_w = 0: tile -1, in slot 1)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) vf[i] = (nt_w & 1) ? vfrag(0, i) : vfrag(1, i);
+    for (int i = 0; i < 8; ++i) vf[i] = vread(last, i);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
