@@ -69,7 +69,8 @@
 // window's edge go through the masking branch, as those at the diagonal do.
 // Tokens of an item's tiles that none of its rows sees are zero in LDS, and a
 // wave takes the V operands of a tile that its own rows do not see from a block
-// of zeros: what is there need not be finite.
+// of zeros, those of the tile with the last sink, once its rows see only the
+// sinks there, from a copy without the others: what is there need not be finite.
 //
 // Block scales (BLK): the copy of a piece multiplies by 2^(e - 127) where it
 // widens e4m3 to bf16, in the same instruction; e is one byte per 2 KiB tile,
@@ -102,7 +103,7 @@ constexpr float kMinusBig = -3.0e38f; // the reference max of a column with no s
 constexpr int kMaxBatch = 4096;
 constexpr int kIdCap = 4096;          // block ids staged in LDS: contexts up to 65,536 tokens
 constexpr int kList = 64;             // rounds of items looked up at once
-constexpr int kMaxPairBatch = 3968;         // (160 KiB less 97.8 KiB) over 16 bytes a sequence, rounded down
+constexpr int kMaxPairBatch = 3424;         // (160 KiB less 106.3 KiB) over 16 bytes a sequence, rounded down
 constexpr int kMaxWindowContext = 1 << 30;  // positions, and a little above, are 32-bit
 constexpr int kWindowRoom = 512;      // tokens of an item's steps beside window and sinks: 255 + 3 * 63, rounded up
 // LDS layout of a sub-tile (byte offsets; a chunk is 16 bytes)
@@ -216,6 +217,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
   // V operands of a tile that a wave's rows do not see (WIN): all its reads, from one base
   constexpr int kZeros = WIN ? 3 * (32 * kVPitch + 128) + 4 * kVPitch + 16 : 16;
   __shared__ __attribute__((aligned(16))) char zero_v[kZeros];
+  // V of the tile with the last sink, the tokens behind it zero (WIN).  (With it two
+  // workgroups of four waves share a unit's LDS up to 721 sequences.)
+  __shared__ __attribute__((aligned(16))) char sink_v[WIN ? kVSlot : 16];
   extern __shared__ int tile_pre[];  // [B + 1] items per KV head of sequences 0..s-1, then r0[B], r1[B], T[B]
 
   const int tid = threadIdx.x;
@@ -371,11 +375,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     const int nt_w = c0 + cg * kWaveCols >= ncols || p_end < kKT * ks ? 0 : from((p_end - kKT * ks) / ST + 1);
     // (WIN) the first and the last column's window begin here
     const int lo_first = pmin - a.window + 1, lo_last = p_end - a.window + 1;
-    // the wave sees nothing of step j
-    auto hidden = [&](int j) __attribute__((always_inline)) {
-      const int t0 = ST * real(j) + kKT * ks;
-      return WIN && t0 + kKT <= lo_first && t0 >= a.n_sink;
-    };
+    // (WIN) The step of the tile that holds the last sink and tokens behind it, if
+    // the item's first row sees some of these and the window of its last has passed
+    // them all; -1: no copy of it is needed (what no row sees is zero in the tile).
+    const int sink_t0 = WIN ? a.n_sink & ~(kKT - 1) : 0, sink_end = sink_t0 + kKT;
+    const int j_sink =
+        WIN && sink_t0 != a.n_sink && lo < sink_end && T - n + tok_last - a.window + 1 >= sink_end ? a.n_sink / ST : -1;
 
     float cmul = a.scale_log2, vsc = 1.0f;
     int q_sign = 0;
@@ -525,6 +530,22 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
 #pragma unroll
     for (int x = 0; x < 8; ++x) ones[x] = (__bf16)1.0f;
 
+    // (Here, and not where the loop stores the tile: there it would be code in every
+    // step.  70 sequences of eight rows, window 256, 64/8 heads: without it 32.8 us,
+    // 33.6 so; prompts, window 128, 138.8 and 139.8; long windows and pairs of waves
+    // the same.)
+    if (WIN && j_sink >= 0) {
+      Ids id, t;
+      read_ids(j_sink, id);
+      bases(id, t);
+      Chunk r;
+      load(a.v, a.v_exp, voff_g, t, r);
+#pragma unroll
+      for (int x = 0; x < S * NL; ++x)
+        if (ST * real(j_sink) + kKT * (x / NL) == sink_t0)
+          *(i32x4*)(sink_v + vdst + (32 * kVPitch + 128) * (x % NL)) =
+              zero_tokens_from(widen(r, x), sink_t0 + 16 * cb + 8 * (lane & 1), a.n_sink);
+    }
     // K tiles 0 and 1 to LDS; K tiles 2, 3 and V tiles 0, 1 in registers
     Chunk kA, vA, kB, vB;
     Ids idn, tb[2];  // ids of K tile j + 4; bases of tiles j + 2, j + 3
@@ -559,9 +580,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     auto vread = [&](const char* base, int nn) __attribute__((always_inline)) {
       return *(const i32x4*)(base + (32 * kVPitch + 128) * (nn >> 1) + 4 * kVPitch * (nn & 1));
     };
-    // V of tile j, which is in `slot`: zeros where the wave sees nothing of it
+    // V of tile j, which is in `slot`: once the wave's windows have passed it, zeros, or what sinks it holds
     auto vtile = [&](int j, int slot) __attribute__((always_inline)) {
-      return hidden(j) ? (const char*)zero_v : vbase(slot);
+      const int t0 = ST * real(j) + kKT * ks;
+      if (!WIN || t0 + kKT > lo_first || t0 + kKT <= a.n_sink) return vbase(slot);
+      return t0 >= a.n_sink ? (const char*)zero_v : j_sink >= 0 ? (const char*)sink_v + vro : vbase(slot);
     };
     struct Scores { f32x4 z[NC][2]; };       // [column block][m]: tokens 8 lj + 4 m + e
     struct Probs { i32x4 p[NC]; };
@@ -670,8 +693,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
     // first step with a token past some column's position in its scores, or
     // past the sequence's end in the V tile it writes
     const int j_rare = from(min((pmin + 1 - kKT * ks) / ST, T / ST));
-    // (WIN) steps before this one may hold tokens that some column's window has passed
-    const int j_left = WIN ? from((max(lo_last, 0) + ST - 1) / ST) : 0;
+    // (WIN) steps before this one may hold tokens that some column's window has
+    // passed, or multiply V of a tile that the wave's windows have passed
+    const int j_left = WIN && lo_last > 0 ? from(lo_last / ST + S) : 0;
     // One step: scores of tile j+1, output products of tile j-1 and
     // probabilities of tile j, independent of one another, in sixteen slots
     // of four matrix products each.
@@ -679,11 +703,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_kernel(PrefillArgs a) 
                     __attribute__((always_inline)) {
 #pragma unroll
       for (int f = 0; f < 4; ++f) kf[f] = kfrag(par ^ 1, f);
-      const char* const vb = vtile(j - 1, par ^ 1);
+      const char* vb = vbase(par ^ 1);
       bool grown = false;
       if (j >= j_rare || (WIN && j < j_left) || __builtin_amdgcn_ballot_w64(over > 0.f) != 0) {
         grown = prepare(j, cur);
         clip_v(j, vr);
+        vb = vtile(j - 1, par ^ 1);
       }
       Ids t4;
       float z0 = __builtin_fmaf(cur.z[0][0][0], cmul, -mc[0]), z1 = __builtin_fmaf(cur.z[0][0][1], cmul, -mc[0]);

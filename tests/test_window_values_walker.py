@@ -4,7 +4,9 @@ A token that a column does not see has probability 0 there, and 0 times a value
 that is not finite is not.  This restates which V tile a wave takes for each of
 its steps, the last one's read behind the loop included (vtile), and what is
 zeroed in the tiles for all waves (clip_v), and checks that a token's value
-meets only columns within 62 positions of a row that sees it.
+meets only columns within 62 positions of a row that sees it, and that the
+copy of the tile with the last sink is made in every item where a wave reads it,
+and that the steps that choose another V tile take the branch that does so.
 
 A kernel change to any of these must be mirrored here.
 """
@@ -14,11 +16,11 @@ import pytest
 KT = 32
 
 
-def v_of(t0, lo_first, n_sink):
+def v_of(t0, lo_first, n_sink, copied):
     """The tokens of the tile at t0 whose values a wave takes: its window's first token is lo_first."""
-    if t0 + KT <= lo_first and t0 >= n_sink:      # hidden: a block of zeros
-        return t0, t0
-    return t0, t0 + KT
+    if t0 + KT > lo_first or t0 + KT <= n_sink or t0 < n_sink and not copied:
+        return t0, t0 + KT
+    return t0, max(t0, n_sink)                    # a block of zeros, or the copy of the last sink's tile
 
 
 def furthest(T, n, G, window, n_sink, waves, nc, s):
@@ -33,7 +35,11 @@ def furthest(T, n, G, window, n_sink, waves, nc, s):
         gap = lo // st - head
         real = lambda j: j + gap if j >= head else j  # noqa: B023, E731
         frm = lambda r: r if r <= head else max(r - gap, head)  # noqa: B023, E731
-        assert -(-n_kv // st) - gap > 0
+        nt = -(-n_kv // st) - gap
+        sink_t0 = n_sink // KT * KT
+        last = T - n + tok_last - window + 1
+        j_sink = n_sink // st if sink_t0 != n_sink and lo < sink_t0 + KT <= last else -1
+        assert j_sink < 0 or j_sink < nt and real(j_sink) == n_sink // st
         for w in range(waves):
             ks, cg = w % s, w // s
             if c0 + cg * wave_cols >= ncols:
@@ -41,8 +47,16 @@ def furthest(T, n, G, window, n_sink, waves, nc, s):
             pmin = T - n + min(c0 + cg * wave_cols, ncols - 1) // G
             p_end = T - n + (min(c0 + (cg + 1) * wave_cols, ncols) - 1) // G
             nt_w = 0 if p_end < KT * ks else frm((p_end - KT * ks) // st + 1)
+            lo_last = p_end - window + 1
+            j_left = frm(lo_last // st + s) if lo_last > 0 else 0
+            # (the steps of tokens that some column's window has passed, which the masks ask for)
+            assert j_left >= frm((max(lo_last, 0) + st - 1) // st)
             for j in range(nt_w):
-                first, end = v_of(st * real(j) + KT * ks, pmin - window + 1, n_sink)
+                first, end = v_of(st * real(j) + KT * ks, pmin - window + 1, n_sink, j_sink >= 0)
+                if end < first + KT:              # chosen in the branch for the steps before j_left, or behind the loop
+                    assert j == nt_w - 1 or j + 1 < j_left
+                if first < end < first + KT:
+                    assert first == sink_t0 and j == j_sink
                 for x in range(first, min(end, T)):
                     if n_sink <= x < lo:
                         continue                  # zero in the tile
@@ -62,7 +76,8 @@ def test_values_stay_near(waves, nc, s):
     for _ in range(40):
         T = int(rng.integers(1, 900))
         trials.append((T, int(rng.integers(1, T + 1)), int(rng.choice([1, 2, 8])), int(rng.integers(1, 300)),
-                       int(rng.choice([0, 32, 64, 96, 192]))))
-    worst = max(furthest(T, n, G, min(window, T), min(n_sink, T // KT * KT), waves, nc, s)
+                       int(rng.choice([0, 1, 4, 31, 32, 40, 64, 77, 96, 192]))))
+    trials += [(600, 600, 1, 100, k) for k in (1, 8, 33, 48, 63)]
+    worst = max(furthest(T, n, G, min(window, T), min(n_sink, T), waves, nc, s)
                 for T, n, G, window, n_sink in trials)
     assert 0 < worst <= 62
