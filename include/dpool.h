@@ -354,7 +354,8 @@ int paged_decode_attention_noalloc(const void* q, const void* k_blocks, const vo
 /* A cached value of a token that is not seen never reaches the result,      */
 /* finite or not, and table entries of blocks that hold no token that is     */
 /* seen are never read (blocks that have left the window may go back to the  */
-/* pool).  window >= 1; one of max_context_len or more hides nothing.        */
+/* pool, their entries set below 0; kv_tables_step then ends such a sequence  */
+/* with -2).  window >= 1; one of max_context_len or more hides nothing.      */
 /* n_sink >= 0.                                                               */
 /*                                                                           */
 /* kv_dtype may also be DP_KV_FP8_E4M3_BLOCK: the cache holds e4m3 codes as  */
@@ -506,7 +507,11 @@ int window_prefill_attention(const void* q, const void* k_blocks, const void* v_
 /*     x < 0   the sequence is over: its b table entries go to the end of   */
 /*             the ring, in table order, sequences in batch order; its      */
 /*             context and owned count become 0 (they are free for the next */
-/*             call, not for this one)                                       */
+/*             call, not for this one).  With x = -1 all b entries go, with  */
+/*             x < -1 those that are not below 0: a sequence whose blocks    */
+/*             left a window earlier, and went back to the ring then with    */
+/*             their entries set below 0, ends with x = -2.  Such entries    */
+/*             count as owned                                                */
 /*     x >= 0  it needs max(0, ceil((c + x) / 16) - b) blocks.  In batch    */
 /*             order, needs are met while the sum of all needs so far is at */
 /*             most `count`; a sequence that needs none is always met.      */

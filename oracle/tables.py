@@ -40,8 +40,9 @@ def step(ctx, owned, new, ring, head, count, tables, total_rows, parents=None, w
         b = max(int(owned[s]), -(-c // BS))
         if x < 0:
             for j in range(b):
-                ring[(head + count + gave) % nb] = tables[s, j]
-                gave += 1
+                if tables[s, j] >= 0 or x == -1:   # (below -1: entries below 0 hold no block)
+                    ring[(head + count + gave) % nb] = tables[s, j]
+                    gave += 1
             out["ctx"].append(0)
             out["owned"].append(0)
             out["granted"].append(1)

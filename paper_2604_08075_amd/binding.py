@@ -490,7 +490,8 @@ def tables_shape(batch, max_blocks_per_seq, num_blocks, total_rows, mask_words=0
 def kv_tables_step(context_lens, n_owned, new_tokens, free_ids, free_state, block_tables, context_lens_out,
                    n_owned_out, free_state_out, q_start, slots, positions, granted, shape: TablesShape, parents=None,
                    tree_mask=None, stream=None) -> None:
-    """Enqueue one step of the block tables (include/dpool.h, kv_tables_step)."""
+    """Enqueue one step of the block tables (include/dpool.h, kv_tables_step); new_tokens -1 ends a sequence, -2 one
+    whose entries below 0 hold no block."""
     check(lib().kv_tables_step(
         context_lens.data_ptr(), n_owned.data_ptr(), new_tokens.data_ptr(),
         parents.data_ptr() if parents is not None else None, free_ids.data_ptr(), free_state.data_ptr(),

@@ -17,6 +17,13 @@
 // and wave sums by permutes instead of two and lane shifts 1.2, 0.5 and 1.6 more.
 // A row's sequence is found by a binary search over the running sums in LDS.
 //
+// Where a sequence that is over may have entries without a block (its blocks left
+// a window), an entry's place in the ring depends on all before it: then one
+// workgroup counts its way through the entries.  (Looking for such entries in
+// every call, which each workgroup with a share would do for all of them, took
+// 33 us instead of 6 where 256 sequences of 1,400 tokens end, so the caller says
+// which sequences they are.)
+//
 // Nothing that the call reads is written by it (the ring's tail and the table
 // entries behind the owned ones are not read), so workgroups need no order.
 #include <hip/hip_runtime.h>
@@ -33,11 +40,12 @@ constexpr int kMaxBatch = 4096;
 constexpr int kMaxWords = 4;
 constexpr int64_t kMaxCount = (int64_t)1 << 30;  // rows and blocks: two such counts add up in 32 bits
 constexpr int kMaxThreads = 512;
+constexpr int kPer = 4;  // entries that a thread counts in a turn
 
 struct TablesArgs {
   const int32_t* context;
   const int32_t* owned;
-  const int32_t* fresh;    // new tokens, < 0: the sequence is over
+  const int32_t* fresh;    // new tokens, < 0: the sequence is over, < -1: and entries below 0 hold no block
   const int32_t* parents;  // [rows] or null
   int32_t* ring;           // [num_blocks]
   const int32_t* state_in;
@@ -96,10 +104,11 @@ __device__ __forceinline__ int find(const uint32_t* start, int n, uint32_t i) {
 }
 
 __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
-  // [B + 1] first row, [B + 1] first released block, [B] first new block of
-  // the ring (~0: refused), [threads] + 256 parents of the rows at hand
+  // [B + 1] first row, [B + 1] first released entry, [B] first new block of
+  // the ring (~0: refused; of a sequence that is over: 1 if entries below 0 hold
+  // no block), [threads] + 256 parents of the rows at hand
   extern __shared__ uint32_t lds[];
-  __shared__ uint32_t wsum[3][kMaxThreads / 64], took;
+  __shared__ uint32_t wsum[3][kMaxThreads / 64], took, gaps;  // gaps: entries below 0 may be among the released
   const int B = a.batch, tid = threadIdx.x, nt = blockDim.x;
   uint32_t* const row0 = lds;
   uint32_t* const back0 = row0 + B + 1;
@@ -112,7 +121,7 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
   const uint32_t free = min((uint32_t)max(a.state_in[1], 0), nb);
 
   uint32_t rows_c = 0, back_c = 0, need_c = 0;  // sums of the chunks before
-  if (tid == 0) row0[0] = back0[0] = took = 0;
+  if (tid == 0) row0[0] = back0[0] = took = gaps = 0;
   int x1 = 0, c1 = 0, b1 = 0;  // a chunk ahead
   if (tid < B) x1 = a.fresh[tid], c1 = a.context[tid], b1 = a.owned[tid];
   for (int base = 0; base < B; base += nt) {
@@ -124,10 +133,10 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
     c = (int)min((int64_t)max(c, 0), cap);
     b = max(min(max(b, 0), a.max_blocks), (int)((uint32_t)(c + kBS - 1) / kBS));
     const uint32_t n_upto = wave_scan(n, a.rows + 1, wsum[0]);
-    const uint32_t back_upto = wave_scan(x < 0 ? (uint32_t)b : 0, nb, wsum[1]);
+    const uint32_t back_upto = wave_scan(x < 0 ? (uint32_t)b : 0, kMaxCount, wsum[1]);
     __syncthreads();
     const uint32_t rows_end = join_waves(n_upto, a.rows + 1, wsum[0], rows_c);
-    const uint32_t back_end = join_waves(back_upto, nb, wsum[1], back_c);
+    const uint32_t back_end = join_waves(back_upto, kMaxCount, wsum[1], back_c);
     const int64_t want = (int64_t)c + n;
     const bool fits = want <= cap && rows_end <= a.rows && !(a.parents && n > 64u * a.words);
     const uint32_t need = fits && x > 0 ? (uint32_t)max((int64_t)0, (want + kBS - 1) / kBS - b) : 0;
@@ -138,7 +147,8 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
     if (s < B) {
       row0[s + 1] = min(rows_end, a.rows);
       back0[s + 1] = back_end;
-      take0[s] = ok ? need_end - need : ~0u;
+      take0[s] = x < 0 ? x < -1 : ok ? need_end - need : ~0u;
+      if (x < -1) gaps = 1;
       if (blockIdx.x == 0) {
         a.granted[s] = ok || x < 0;
         a.context_out[s] = x < 0 ? 0 : ok ? (int)want : c;
@@ -150,20 +160,56 @@ __global__ __launch_bounds__(kMaxThreads) void kv_tables_kernel(TablesArgs a) {
     if (blockIdx.x == 0 && ok && need) atomicMax(&took, need_end);
   }
   __syncthreads();
-  const uint32_t back = min(back_c, nb - free);  // more would overtake the ring's head: ids that were never handed out
+  const uint32_t room = nb - free;  // more would overtake the ring's head: ids that were never handed out
+  uint32_t back = min(back_c, room);
+  const uint32_t rows_used = row0[B];
+
+  // released blocks
+  if (!gaps) {
+    for (uint32_t f = blockIdx.x * nt + tid; f < back; f += gridDim.x * nt) {
+      const int s = find(back0, B, f);
+      uint32_t at = head + free + f;  // below 3 * 2^30
+      at %= nb;
+      a.ring[at] = a.tables[(size_t)s * a.max_blocks + (f - back0[s])];
+    }
+  } else if (blockIdx.x == 0) {
+    uint32_t gave = 0;  // blocks of the entries before
+    for (uint32_t f0 = 0; f0 < back_c; f0 += kPer * nt) {
+      int id[kPer], s = 0;
+      uint32_t n = 0, end = 0;
+      bool gives[kPer];
+#pragma unroll
+      for (int y = 0; y < kPer; ++y) {
+        const uint32_t f = f0 + tid * kPer + y;
+        gives[y] = false;
+        id[y] = 0;
+        if (f < back_c) {
+          if (f >= end) {
+            s = find(back0, B, f);
+            end = back0[s + 1];
+          }
+          id[y] = a.tables[(size_t)s * a.max_blocks + (f - back0[s])];
+          gives[y] = id[y] >= 0 || !take0[s];
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kPer; ++y) n += gives[y];
+      const uint32_t upto = wave_scan(n, kMaxCount, wsum[0]);
+      __syncthreads();
+      uint32_t rank = join_waves(upto, kMaxCount, wsum[0], gave) - n;
+      __syncthreads();  // (the next turn's wsum)
+#pragma unroll
+      for (int y = 0; y < kPer; ++y) {
+        if (gives[y] && rank < room) a.ring[(head + free + rank) % nb] = id[y];
+        rank += gives[y];
+      }
+    }
+    back = min(gave, room);
+  }
   if (blockIdx.x == 0 && tid == 0) {
     a.q_start[0] = 0;
     a.state_out[0] = (int)((head + took) % nb);  // (both below 2^30 + 1)
     a.state_out[1] = (int)(free - took + back);
-  }
-  const uint32_t rows_used = row0[B];
-
-  // released blocks
-  for (uint32_t f = blockIdx.x * nt + tid; f < back; f += gridDim.x * nt) {
-    const int s = find(back0, B, f);
-    uint32_t at = head + free + f;  // below 3 * 2^30
-    at %= nb;
-    a.ring[at] = a.tables[(size_t)s * a.max_blocks + (f - back0[s])];
   }
 
   // rows, a workgroup's threads a chunk
