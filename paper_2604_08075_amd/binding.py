@@ -358,20 +358,34 @@ def _stream_ptr(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _stream_here(stream, a, b):
-    """_stream_ptr, for tensors a and b on the current device, where the launch goes; refuses others."""
+def _stream_here(stream, dev):
+    """_stream_ptr, for tensors on device dev, which has to be the current one, where the launch goes."""
     import torch
-    dev = a.get_device()
-    if dev < 0 or dev != b.get_device():
-        raise ValueError(f"tensors on {a.device} and {b.device}: they must be on the current device")
+    if dev < 0:
+        raise ValueError("tensors must all be on the current device")
     try:
         if dev == torch._C._cuda_getDevice() and stream is None:
             return torch._C._cuda_getCurrentRawStream(dev)
     except AttributeError:  # (as in _stream_ptr)
         pass
     if dev != torch.cuda.current_device():
-        raise ValueError(f"tensors on {a.device}: they must be on the current device")
+        raise ValueError(f"tensors on device {dev}: they must be on the current device")
     return _stream_ptr(stream)
+
+
+_types = None
+
+
+def _element_types():
+    """The element types that may hold bf16 values, e4m3 codes and exponent bytes (as such or as their bits); int32,
+    int64 and float32."""
+    global _types
+    if _types is None:
+        import torch
+        some = lambda *names: frozenset(getattr(torch, n) for n in names if hasattr(torch, n))  # noqa: E731
+        _types = (some("bfloat16", "int16", "uint16"), some("float8_e4m3fn", "uint8", "int8"),
+                  some("float8_e8m0fnu", "uint8", "int8"), torch.int32, torch.int64, torch.float32)
+    return _types
 
 
 def _ws(workspace):
@@ -408,34 +422,67 @@ def window_workspace_size(shape: DecodeShape, window, n_sink=0) -> int:
     return int(lib().window_decode_workspace_size(ctypes.byref(shape), window, n_sink))
 
 
-def _check_window(q, k_blocks, v_blocks, block_tables, lens, out, shape, k_scale, v_scale) -> None:
-    """Refuses tensors with gaps, ids that are not int32, scales that are not the cache type's."""
-    # (written out: half of what a loop takes on the host, 0.6 us)
+def _check_window(q, k_blocks, v_blocks, block_tables, lens, out, shape, rows, k_scale, v_scale, more=None,
+                  more_dtype=None) -> int:
+    """Refuses tensors with gaps, of other types than the shape's, with fewer elements than it asks for, or apart.
+    more: the workspace, or the row offsets (of more_dtype).  Returns the tensors' device."""
+    # (written out: half of what a loop takes on the host)
     if not (q.is_contiguous() and k_blocks.is_contiguous() and v_blocks.is_contiguous() and block_tables.is_contiguous()
             and lens.is_contiguous() and out.is_contiguous()):
         raise ValueError("q, caches, block tables, lengths and out must be contiguous")
-    if block_tables.itemsize != 4 or lens.itemsize != 4:
+    bf16, codes, exponents, int32, _, float32 = _element_types()
+    kv, batch, heads = shape.kv_dtype, shape.batch, shape.n_kv_heads
+    cache = codes if kv else bf16
+    if q.dtype not in bf16 or k_blocks.dtype not in cache or v_blocks.dtype not in cache:
+        raise ValueError(f"q is bf16 and the caches are {'e4m3' if kv else 'bf16'}, not {q.dtype}, {k_blocks.dtype} and "
+                         f"{v_blocks.dtype}")
+    if block_tables.dtype is not int32 or lens.dtype is not int32:
         raise ValueError("block tables and lengths are int32")
+    if out.dtype is not float32 if shape.out_dtype else out.dtype not in bf16:
+        raise ValueError(f"out is {'fp32' if shape.out_dtype else 'bf16'}, not {out.dtype}")
+    tiles = shape.num_blocks * heads
+    size, width = tiles * 2048, rows * shape.n_q_heads * 128  # (a tile: 16 tokens of 128 dimensions)
+    if (q.numel() < width or out.numel() < width or k_blocks.numel() < size or v_blocks.numel() < size
+            or block_tables.numel() < batch * shape.max_blocks_per_seq or lens.numel() < batch):
+        raise ValueError("q, caches, block tables, lengths or out have fewer elements than the shape")
+    dev = q.get_device()
+    here = (dev >= 0 and k_blocks.get_device() == dev and v_blocks.get_device() == dev
+            and block_tables.get_device() == dev and lens.get_device() == dev and out.get_device() == dev)
     if k_scale is not None and v_scale is not None:
-        size = 1 if shape.kv_dtype == KV_FP8_E4M3_BLOCK else 4
-        if k_scale.itemsize != size or v_scale.itemsize != size:
+        if (k_scale.dtype not in exponents or v_scale.dtype not in exponents) if kv == KV_FP8_E4M3_BLOCK else (
+                k_scale.dtype is not float32 or v_scale.dtype is not float32):
             raise ValueError("scales are fp32 for each head, or one exponent byte for each block and head")
         if not (k_scale.is_contiguous() and v_scale.is_contiguous()):
             raise ValueError("scales must be contiguous")
+        size = tiles if kv == KV_FP8_E4M3_BLOCK else heads
+        if k_scale.numel() < size or v_scale.numel() < size:
+            raise ValueError(f"scales have {k_scale.numel()} and {v_scale.numel()} elements, the shape asks for {size}")
+        here = here and k_scale.get_device() == dev and v_scale.get_device() == dev
+    if more is not None:
+        if more_dtype is not None and (more.dtype is not more_dtype or more.numel() <= batch):
+            raise ValueError("q_start is int32 and has an element more than the batch")
+        if not more.is_contiguous():
+            raise ValueError("workspace and q_start must be contiguous")
+        here = here and more.get_device() == dev
+    if not here:
+        raise ValueError("tensors must all be on the current device")
+    return dev
 
 
 def window_decode_attention(q, k_blocks, v_blocks, block_tables, context_lens, scale, window, n_sink, out,
                             shape: DecodeShape, workspace=None, k_scale=None, v_scale=None, stream=None) -> None:
     """Enqueue the decode over a sliding window and the first n_sink tokens, or over block scales
-    (include/dpool.h, window_decode_attention).  Tensors have to be contiguous and on the
-    current device (ValueError otherwise)."""
-    _check_window(q, k_blocks, v_blocks, block_tables, context_lens, out, shape, k_scale, v_scale)
+    (include/dpool.h, window_decode_attention).  Tensors, the workspace among them, have to be contiguous, of the
+    shape's element types (or integers of their size, for bf16, e4m3 and exponents), at least as large as it says and
+    on the current device (ValueError otherwise)."""
+    dev = _check_window(q, k_blocks, v_blocks, block_tables, context_lens, out, shape, shape.batch, k_scale, v_scale,
+                        workspace)
     ws_ptr, ws_bytes = _ws(workspace)
     check(lib().window_decode_attention(
         q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
         float(scale), window, n_sink, k_scale.data_ptr() if k_scale is not None else None,
         v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape), ws_ptr, ws_bytes,
-        _stream_here(stream, q, k_blocks)))
+        _stream_here(stream, dev)))
 
 
 def kv_cache_append(k_new, v_new, k_blocks, v_blocks, block_tables, positions, shape: DecodeShape, k_scale=None,
@@ -469,16 +516,16 @@ def chunked_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens,
 def window_prefill_attention(q, k_blocks, v_blocks, block_tables, context_lens, q_start, scale, window, n_sink, out,
                              shape: PrefillShape, k_scale=None, v_scale=None, stream=None) -> None:
     """Enqueue the chunked prefill over a sliding window and the first n_sink tokens, or over block scales
-    (include/dpool.h, window_prefill_attention).  Tensors have to be contiguous and on the
-    current device (ValueError otherwise)."""
-    _check_window(q, k_blocks, v_blocks, block_tables, context_lens, out, shape, k_scale, v_scale)
-    if not q_start.is_contiguous() or q_start.itemsize != 4:
-        raise ValueError("q_start is int32 and contiguous")
+    (include/dpool.h, window_prefill_attention).  Tensors have to be contiguous, of the shape's element types (or
+    integers of their size, for bf16, e4m3 and exponents), at least as large as it says and on the current device
+    (ValueError otherwise)."""
+    dev = _check_window(q, k_blocks, v_blocks, block_tables, context_lens, out, shape, shape.total_q, k_scale, v_scale,
+                        q_start, _element_types()[3])
     check(lib().window_prefill_attention(
         q.data_ptr(), k_blocks.data_ptr(), v_blocks.data_ptr(), block_tables.data_ptr(), context_lens.data_ptr(),
         q_start.data_ptr(), float(scale), window, n_sink, k_scale.data_ptr() if k_scale is not None else None,
         v_scale.data_ptr() if v_scale is not None else None, out.data_ptr(), ctypes.byref(shape),
-        _stream_here(stream, q, k_blocks)))
+        _stream_here(stream, dev)))
 
 
 # ---------------------------------------------------------------- a step that verifies drafted tokens
@@ -575,12 +622,15 @@ def qk_norm_rope_append_scaled(q, k, v, cos_sin, positions, slots, q_out, k_bloc
         raise ValueError("k_scale and v_scale hold one exponent byte for each block and head")
     if positions.itemsize != 4 or slots.itemsize != 8:
         raise ValueError("positions are int32, slots int64")
+    dev = k.get_device()
+    if dev != k_blocks.get_device():
+        raise ValueError("tensors must all be on the current device")
     check(lib().qk_norm_rope_append_scaled(
         q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(),
         q_weight.data_ptr() if q_weight is not None else None, k_weight.data_ptr() if k_weight is not None else None,
         float(eps), cos_sin.data_ptr() if cos_sin is not None else None, positions.data_ptr(), slots.data_ptr(),
         q_out.data_ptr() if q_out is not None else None, k_blocks.data_ptr(), v_blocks.data_ptr(), k_scale.data_ptr(),
-        v_scale.data_ptr(), ctypes.byref(shape), _stream_here(stream, k, k_blocks)))
+        v_scale.data_ptr(), ctypes.byref(shape), _stream_here(stream, dev)))
 
 
 def tree_shape(batch, n_q_heads, n_kv_heads, max_blocks_per_seq, max_context_len, num_blocks, total_q, mask_words=1,
