@@ -608,22 +608,54 @@ def qk_norm_rope_append_scaled(q, k, v, cos_sin, positions, slots, q_out, k_bloc
     qk_norm_rope_append_scaled); k_scale and v_scale, one byte each, are updated with it.
 
     q and q_out may be None where the shape has no query heads.  Rows as for
-    qk_norm_rope_append; caches, scales, positions and slots have to be
-    contiguous and on the current device (ValueError)."""
+    qk_norm_rope_append; all other tensors have to be contiguous.  Element types
+    as the names say, or integers of their size for bf16, e4m3 and exponents
+    (int32 positions, int64 slots, fp32 cos_sin); at least as many elements as
+    the shape asks for; all on the current device (ValueError)."""
+    rows, cells = shape.rows, shape.num_blocks * shape.n_kv_heads
+    width, size = rows * shape.n_kv_heads * 128, cells * 2048  # (a tile: 16 tokens of 128 dimensions)
+    bf16, codes, exponents, int32, int64, float32 = _element_types()
+    dev = k.get_device()
+    here = dev >= 0
     if q is None:
-        _check_rows("k", k, shape.rows, shape.n_kv_heads, shape.head_dim, shape.k_stride)
-        _check_rows("v", v, shape.rows, shape.n_kv_heads, shape.head_dim, shape.v_stride)
+        _check_rows("k", k, rows, shape.n_kv_heads, shape.head_dim, shape.k_stride)
+        _check_rows("v", v, rows, shape.n_kv_heads, shape.head_dim, shape.v_stride)
     else:
+        if q_out is None:
+            raise ValueError("q_out is missing")
         _check_qkv(q, k, v, q_out, shape)
+        q_width = rows * shape.n_q_heads * 128
+        if q.dtype not in bf16 or q_out.dtype not in bf16:
+            raise ValueError("q and q_out are bf16")
+        if q.numel() < q_width or q_out.numel() < q_width:
+            raise ValueError("q or q_out has fewer elements than the shape")
+        here = here and q.get_device() == dev and q_out.get_device() == dev
     if not (k_blocks.is_contiguous() and v_blocks.is_contiguous() and k_scale.is_contiguous()
             and v_scale.is_contiguous() and positions.is_contiguous() and slots.is_contiguous()):
         raise ValueError("caches, scales, positions and slots must be contiguous")
-    if k_scale.itemsize != 1 or v_scale.itemsize != 1:
+    if k.dtype not in bf16 or v.dtype not in bf16 or k_blocks.dtype not in codes or v_blocks.dtype not in codes:
+        raise ValueError("k and v are bf16, the caches e4m3")
+    if k_scale.dtype not in exponents or v_scale.dtype not in exponents:
         raise ValueError("k_scale and v_scale hold one exponent byte for each block and head")
-    if positions.itemsize != 4 or slots.itemsize != 8:
+    if positions.dtype is not int32 or slots.dtype is not int64:
         raise ValueError("positions are int32, slots int64")
-    dev = k.get_device()
-    if dev != k_blocks.get_device():
+    if (k.numel() < width or v.numel() < width or k_blocks.numel() < size or v_blocks.numel() < size
+            or k_scale.numel() < cells or v_scale.numel() < cells or positions.numel() < rows or slots.numel() < rows):
+        raise ValueError("k, v, caches, scales, positions or slots have fewer elements than the shape")
+    here = (here and v.get_device() == dev and k_blocks.get_device() == dev and v_blocks.get_device() == dev
+            and k_scale.get_device() == dev and v_scale.get_device() == dev and positions.get_device() == dev
+            and slots.get_device() == dev)
+    if cos_sin is not None:
+        if (cos_sin.dtype is not float32 or not cos_sin.is_contiguous()
+                or cos_sin.numel() < shape.n_positions * shape.rotary_dim):
+            raise ValueError("cos_sin is fp32, contiguous and has a row for each position")
+        here = here and cos_sin.get_device() == dev
+    for w in (q_weight, k_weight):
+        if w is not None:
+            if w.dtype not in bf16 or not w.is_contiguous() or w.numel() < 128:
+                raise ValueError("q_weight and k_weight are bf16, contiguous and have 128 elements")
+            here = here and w.get_device() == dev
+    if not here:
         raise ValueError("tensors must all be on the current device")
     check(lib().qk_norm_rope_append_scaled(
         q.data_ptr() if q is not None else None, k.data_ptr(), v.data_ptr(),

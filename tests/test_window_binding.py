@@ -109,3 +109,84 @@ def test_attention_types_that_hold_the_same_bits(host_lib, kind, cache):
         for t in types if name in args else ():
             with pytest.raises(ValueError, match="current device"):
                 call(**{name: torch.zeros(args[name].shape, dtype=torch.uint8 if t.itemsize == 1 else torch.int16).view(t)})
+
+
+# ---------------------------------------------------------------- the cache write
+
+def write(lib, queries=True):
+    """(call, its arguments): the write of four rows into a cache with block scales."""
+    hq = HQ if queries else 0
+    args = dict(k=torch.zeros((4, HKV, 128), dtype=torch.bfloat16), v=torch.zeros((4, HKV, 128), dtype=torch.bfloat16),
+                cos_sin=torch.zeros((20, 128)), positions=torch.zeros(4, dtype=torch.int32),
+                slots=torch.zeros(4, dtype=torch.int64), k_blocks=torch.zeros((NB, HKV, 16, 128), dtype=torch.uint8),
+                v_blocks=torch.zeros((NB, HKV, 128, 16), dtype=torch.uint8),
+                k_scale=torch.zeros((NB, HKV), dtype=torch.uint8), v_scale=torch.zeros((NB, HKV), dtype=torch.uint8),
+                k_weight=torch.zeros(128, dtype=torch.bfloat16))
+    if queries:
+        args.update(q=torch.zeros((4, HQ, 128), dtype=torch.bfloat16), q_out=torch.zeros((4, HQ, 128), dtype=torch.bfloat16),
+                    q_weight=torch.zeros(128, dtype=torch.bfloat16))
+    shape = lib.qk_shape(4, hq, HKV, NB, 20, block_scales=True)
+    none = {} if queries else dict(q=None, q_out=None)
+    return (lambda **more: lib.qk_norm_rope_append_scaled(**dict(dict(args, shape=shape, **none), **more))), args
+
+
+@pytest.mark.parametrize("queries", [True, False])
+def test_write_tensors_elsewhere(host_lib, queries):
+    call, args = write(host_lib, queries)
+    on = {n: Stub(t) for n, t in args.items()}
+    for name in args:
+        for dev in (-1, 1):
+            with pytest.raises(ValueError, match="current device"):
+                call(**dict(on, **{name: Stub(args[name], dev)}))
+    with pytest.raises(ValueError, match="current device"):
+        call()
+
+
+@pytest.mark.parametrize("queries", [True, False])
+def test_write_other_types(host_lib, queries):
+    call, args = write(host_lib, queries)
+    wrong = dict.fromkeys(("q", "q_out", "k", "v", "q_weight", "k_weight"), (torch.float16, torch.float32, torch.uint8))
+    wrong.update(dict.fromkeys(("k_blocks", "v_blocks"), (torch.bfloat16, torch.float8_e5m2, torch.float8_e4m3fnuz)))
+    wrong.update(dict.fromkeys(("k_scale", "v_scale"), (torch.float32, torch.bool, torch.float8_e4m3fn)))
+    wrong.update(cos_sin=(torch.float64, torch.bfloat16, torch.int32), positions=(torch.int64, torch.float32),
+                 slots=(torch.int32, torch.float64))
+    for name, types in wrong.items():
+        for t in types if name in args else ():
+            with pytest.raises(ValueError, match="bf16|fp32|int32|exponent"):
+                call(**{name: torch.zeros(args[name].shape, dtype=t)})
+
+
+@pytest.mark.parametrize("queries", [True, False])
+def test_write_tensors_that_are_too_small(host_lib, queries):
+    call, args = write(host_lib, queries)
+    for name, t in args.items():
+        small = t[:-1] if name in ("q", "q_out", "k", "v") else t.flatten()[:-1]
+        with pytest.raises(ValueError, match="elements|row for each"):
+            call(**{name: small})
+        with pytest.raises(ValueError, match="elements|row for each"):
+            call(**{name: t[:0]})
+
+
+@pytest.mark.parametrize("queries", [True, False])
+def test_write_tensors_with_gaps(host_lib, queries):
+    call, args = write(host_lib, queries)
+    for name, t in args.items():
+        with pytest.raises(ValueError, match="contiguous|strides"):
+            call(**{name: torch.zeros((*t.shape, 2), dtype=t.dtype)[..., 0]})
+
+
+def test_write_without_an_output(host_lib):
+    call, _ = write(host_lib)
+    with pytest.raises(ValueError, match="q_out"):
+        call(q_out=None)
+
+
+def test_write_types_that_hold_the_same_bits(host_lib):
+    call, args = write(host_lib)
+    same = dict.fromkeys(("q", "q_out", "k", "v", "q_weight", "k_weight"), (torch.int16, torch.uint16))
+    same.update(dict.fromkeys(("k_blocks", "v_blocks"), (torch.int8, torch.float8_e4m3fn)))
+    same.update(dict.fromkeys(("k_scale", "v_scale"), (torch.int8, torch.float8_e8m0fnu)))
+    for name, types in same.items():
+        for t in types:
+            with pytest.raises(ValueError, match="current device"):
+                call(**{name: torch.zeros(args[name].shape, dtype=torch.uint8 if t.itemsize == 1 else torch.int16).view(t)})
