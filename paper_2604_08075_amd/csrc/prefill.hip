@@ -1109,17 +1109,19 @@ int enqueue(const void* q, const void* k_blocks, const void* v_blocks, const int
   //  lists of more than kMaxPairBatch sequences.
   const bool may_be_long = win ? seen > 2048 && sh->batch <= kMaxPairBatch : sh->max_context_len > 2048;
   //  - Few rows over a short window: at window_rows.
-  //  - With a window of at most 768 tokens an item has few steps, and what it
+  //  - With a window of at most 768 tokens, 1,280 with the sinks, an item has few steps, and what it
   //    costs before and after them counts: two workgroups of 128 columns on a unit
   //    fill each other's (64/8 heads, eleven prompts of 10,394 tokens in all, then
   //    four chunks of 2,048: window 128, 162 -> 146 and 131 -> 121 us; window 512,
   //    213 -> 207 and 208 -> 203; window 1,024, 254 -> 250 and 320 -> 326; window
-  //    2,048, 298 -> 309 and 562 -> 585).
+  //    2,048, 298 -> 309 and 562 -> 585).  Sinks are steps too (the chunks, 256 ->
+  //    128 columns: window 128 behind 704 sinks 286 -> 276, 1,024 360 -> 359, 4,096
+  //    1,070 -> 1,104; window 512 behind 1,024 442 -> 451, 4,096 1,133 -> 1,165).
   const bool few = win && dpool::window_rows(q, k_blocks, v_blocks, block_tables, context_lens, q_start, scale, a.window,
                                              a.n_sink, k_scale, v_scale, out, sh, stream);
   if (few)
     ;
-  else if (full(256) >= cus && !(win && win->window <= 768))
+  else if (full(256) >= cus && !(win && win->window <= 768 && win->n_sink <= 1280 - win->window))
     launch<8, 2, 1>(a, cache, cus, st);
   else if (full(128) > cus)
     launch<4, 2, 1>(a, cache, 2 * cus, st);

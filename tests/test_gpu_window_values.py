@@ -140,3 +140,19 @@ def test_the_lists_of_large_batches(gpu_lib, batch):
     for fmt, window in (("bf16", 3000), ("e4m3_block", 20)):
         c = Case(rng, ctx, rows, 2, 1, fmt, window, 3, max_blocks=200)
         wc.check(wc.prefill(gpu_lib, c, max_ctx=3200), *c.oracle())
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("window,n_sink", [(768, 512), (768, 513), (769, 0), (5, 1275), (5, 1276)])
+def test_lines_of_short_windows(gpu_lib, fmt, window, n_sink):
+    """Items of 128 columns up to 768 tokens of window and 1,280 with the sinks, of 256 beyond."""
+    note(f"window prefill {fmt}, window {window} and {n_sink} sinks")
+    rng = np.random.default_rng(5)
+    c = Case(rng, [1500] * 4, [256] * 4, 64, 64, fmt, window, n_sink)
+    out = wc.prefill(gpu_lib, c, max_ctx=16 * c.max_blocks)
+    one = Case.__new__(Case)
+    one.__dict__.update(c.__dict__)
+    one.q, one.k, one.v = c.q[:, 33:34], c.k[:, 33:34], c.v[:, 33:34]
+    if fmt != "bf16":
+        one.ks, one.vs = (x[:, 33:34] if fmt == "e4m3_block" else x[33:34] for x in (c.ks, c.vs))
+    wc.check(out[:, 33:34].contiguous(), *one.oracle())
