@@ -649,7 +649,8 @@ int qk_norm_rope_append(const void* q, const void* k, const void* v, const void*
 /* rising, as kv_tables_step hands them out, and nothing else writes to the  */
 /* block meanwhile; V tiles are written whole.  Rows that break this leave   */
 /* unspecified values in their blocks, and no access leaves the buffers.     */
-/* Chains of drafts that are refused are simply written over; drafted trees, */
+/* Chains of drafts that are refused are simply written over (a scale that   */
+/* they raised stays raised for the block's earlier tokens); drafted trees,  */
 /* whose accepted tokens move (kv_cache_accept), need one of the other       */
 /* cache types.                                                               */
 /* n_q_heads may be 0 (q, q_weight, q_out NULL): K and V only, which with     */
